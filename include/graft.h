@@ -19,6 +19,14 @@
  *     graft_matrix_update    refresh of the matrix rows from the verification logits
  *     graft_kv_compact       cache update: the accepted path becomes an ordinary prefix
  *
+ * and, between the target model's projections and its attention, the cache itself:
+ *
+ *     graft_kv_append        rotates queries and keys by position, writes keys and values to the cache
+ *     graft_kv_append_mx     the same into a cache of 4-bit elements
+ *     graft_tree_attn_mx     the attention over it, with capped or windowed scores where a model has them
+ *     graft_kv_compact_mx    its update after acceptance
+ *     graft_kv_gather_mx     its rows as numbers
+ *
  * Conventions shared by every call
  *  - All tensor pointers are DEVICE pointers owned by the caller.  The library
  *    never allocates, frees or keeps them.  Scratch memory comes from
@@ -407,6 +415,116 @@ int32_t graft_prune_select(const int32_t* parent, const int32_t* tokens, const f
                            const int32_t* chk_ret, int32_t n_chk,
                            int32_t* out_parent, int32_t* out_tokens, int32_t* out_index, int32_t* out_n_nodes,
                            int32_t* stage, int32_t* n_ret, int32_t* status, void* stream);
+
+/*
+ * graft_kv_append - what comes between a layer's projections and its attention: queries and
+ * keys are rotated by their position ids (the ones of graft_build_tree_mask: prefix plus
+ * depth, Sec. 3.3), keys and values go to their slots of the paged cache.
+ *
+ * Token i < n_nodes[b] of sequence b has position t = pos[b,i] (pos == NULL: P + i) and slot
+ * P + i, P = prefix_len[b].  With R = rot_dim, pair j < R/2 of a row x is (x[j], x[j+R/2]), or
+ * (x[2j], x[2j+1]) where interleaved != 0, and
+ *     (a, b) -> (a cos - b sin, b cos + a sin),  cos = cos_sin[t,j], sin = cos_sin[t,R/2+j]
+ * for every head of q and k: products and sum each rounded to fp32, then to the storage type.
+ * Elements from R on, and values, stay as they are.
+ *
+ *     q [B,T,Hq,D], k, v [B,T,Hkv,D]   dtype elements; heads of a token dense, the tokens (b T + i)
+ *                        q_stride, k_stride, v_stride elements apart (slices of one fused
+ *                        projection: (Hq + 2 Hkv) D).  Hq = 0 and q = q_out = NULL: keys and values only
+ *     cos_sin [n_pos,R]  fp32, cosines then sines (whatever scaling of frequencies a model has is
+ *                        in the table); NULL with R = 0
+ *     k_cache, v_cache, strides, block_table, prefix_len   as in graft_tree_attn, IN/OUT
+ *     n_nodes [B]        0 <= n_nodes[b] <= T: lengths of a padded batch
+ *     q_out [B,T,Hq,D]   dense; may be q itself where q is dense, and overlaps nothing else
+ * T is not bounded by GRAFT_MAX_NODES: prompts are appended by the same call.  Rows of q_out and
+ * slots of tokens past n_nodes[b] are left as they were.
+ * status [B]: GRAFT_STATUS_BAD_LENGTH if prefix_len or n_nodes is out of range or the tokens
+ * exceed the block table (then nothing of the sequence is written), or if a position lies outside
+ * [0,n_pos) (then nothing of that token is).
+ *
+ * Requires D in {64,128}, R a multiple of 16 and at most D, page_size == GRAFT_PAGE_SIZE, strides that are
+ * multiples of 16 bytes, q, k, v, q_out and caches 16-byte aligned.
+ */
+int32_t graft_kv_append(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                        const float* cos_sin, int32_t n_pos, int32_t rot_dim, int32_t interleaved, const int32_t* pos,
+                        void* k_cache, void* v_cache, int64_t page_stride, int64_t token_stride, int64_t head_stride,
+                        const int32_t* block_table, int32_t max_pages, const int32_t* prefix_len, const int32_t* n_nodes,
+                        int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t page_size, int32_t dtype,
+                        void* q_out, int32_t* status, void* stream);
+
+/*
+ * The 4-bit cache.  Elements are e2m1 (sign, two bits of exponent, one of mantissa: 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6) in blocks of 32 along D with one scale 2^(byte - 127) each; 255 makes NaN of its block.
+ * The 16 tokens that a page holds of one KV head are one run of GRAFT_MX_RUN_BYTES(D) bytes: 8 D
+ * bytes of elements, two to a byte, the one of the smaller index in the low half, then D/32 rows of 16 scale bytes, one
+ * per token.  Order of a run's elements: keys [token][D]; values [token / 4][part of 16][token % 4]
+ * [D/16 elements of the part].  The run of page p and head g starts p*page_stride + g*head_stride BYTES
+ * into the cache (layer l: l*layer_stride more); strides are multiples of 16, caches 16-byte aligned.
+ */
+#define GRAFT_MX_RUN_BYTES(D) (17 * (D) / 2)
+
+/*
+ * graft_kv_append_mx - graft_kv_append into a 4-bit cache.  Rotated keys (in fp32, not rounded to
+ * dtype) and values become blocks: m 2^E being the largest magnitude, the scale is 2^(E-2), 2^(E-1) where m > 1.75, its
+ * byte held within 2..252; elements are rounded to nearest, ties to even, at most 6.  A block with an
+ * infinity or NaN gets the scale byte 255.  q_out is of dtype.
+ */
+int32_t graft_kv_append_mx(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                           const float* cos_sin, int32_t n_pos, int32_t rot_dim, int32_t interleaved, const int32_t* pos,
+                           void* k_cache, void* v_cache, int64_t page_stride, int64_t head_stride,
+                           const int32_t* block_table, int32_t max_pages, const int32_t* prefix_len, const int32_t* n_nodes,
+                           int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t page_size, int32_t dtype,
+                           void* q_out, int32_t* status, void* stream);
+
+/*
+ * graft_kv_gather_mx - rows of a 4-bit cache as numbers: k_out, v_out [n_layers,B,T,Hkv,D] of dtype (both
+ * types hold every element exactly), row t < count[b] being token start[b] + t (start == NULL: t), rows
+ * behind it zeros.  status [B]: GRAFT_STATUS_BAD_LENGTH if start < 0, count outside [0,T] or tokens
+ * exceed the block table; then all rows of the sequence are zeros.
+ */
+int32_t graft_kv_gather_mx(const void* k_cache, const void* v_cache, int64_t layer_stride, int32_t n_layers, int64_t page_stride,
+                           int64_t head_stride, const int32_t* block_table, int32_t max_pages, const int32_t* start,
+                           const int32_t* count, int32_t B, int32_t T, int32_t Hkv, int32_t D, int32_t dtype, void* k_out,
+                           void* v_out, int32_t* status, void* stream);
+
+/*
+ * graft_tree_attn_mx - graft_tree_attn over a 4-bit cache.  For sequence b, node i < n_nodes[b], query head h (KV head
+ * g = h / (Hq/Hkv)), with x_t = scale * q[b,i,h,:] . k_t[g,:]:
+ *     S   = {prefix tokens 0..P-1} U {tree slot j < n_nodes[b] : bit j of mask[b,i] set}
+ *     out[b,i,h,:] = sum_{t in S} softmax_t(y_t) v_t[g,:],   y_t = softcap > 0 ? softcap tanh(x_t / softcap) : x_t
+ * and with window > 0 only those t of S whose position is more than pos[b,i] - window; a prefix token's
+ * position is t, a tree slot's pos[b,j].  Where nothing is left the row is zeros.  mask == NULL: the nodes are a
+ * chain, slot j is seen by nodes i >= j (a single token, a piece of a prompt).  pos is looked at with window > 0 only, where it
+ * may be NULL without a mask: P + i.
+ *
+ * q, out [B,K_max,Hq,D] are bf16.  Queries enter the matrix cores as the sum of three 6-bit numbers: what is
+ * left out of an element is up to 2^-14 of the largest of its 32; probabilities are rounded to bf16; sums are
+ * fp32.  Rows of padding nodes are zeros, and so are all rows of a sequence whose prefix_len < 0,
+ * n_nodes is outside [0,K_max] or tokens exceed the block table.  A key or value block that is NaN makes NaN of
+ * elements of the rows that see its token, and of no other row.
+ *
+ * workspace: at least graft_tree_attn_mx_workspace_bytes(...) bytes (0: NULL will do), 16-byte aligned, scratch; calls that may
+ * run at the same time need one each.  It depends on the current device, as graft_tree_attn_workspace_bytes does.
+ *
+ * Requires D in {64,128}, Hq % Hkv == 0, Hq/Hkv <= 16, 1 <= K_max <= GRAFT_MAX_NODES, 1 <= max_pages <= 262144,
+ * window >= 0, softcap >= 0 and finite, scale finite, q and out 16-byte aligned.
+ */
+size_t graft_tree_attn_mx_workspace_bytes(int32_t B, int32_t K_max, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_pages);
+
+int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const void* v_cache, int64_t page_stride, int64_t head_stride,
+                           const int32_t* block_table, int32_t max_pages, const int32_t* prefix_len, const int32_t* n_nodes,
+                           const uint64_t* mask, const int32_t* pos, int32_t B, int32_t K_max, int32_t Hq, int32_t Hkv, int32_t D,
+                           int32_t page_size, float scale, float softcap, int32_t window, void* out, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/*
+ * graft_kv_compact_mx - graft_kv_compact for a 4-bit cache: the same arguments (strides in bytes), conditions and
+ * status.  new_prefix_len overlaps neither prefix_len nor accept_len.
+ */
+int32_t graft_kv_compact_mx(void* k_cache, void* v_cache, int64_t layer_stride, int32_t n_layers, int64_t page_stride,
+                            int64_t head_stride, const int32_t* block_table, int32_t max_pages, const int32_t* prefix_len,
+                            const int32_t* path, const int32_t* accept_len, int32_t B, int32_t depth_cap, int32_t K_max, int32_t Hkv,
+                            int32_t D, int32_t* new_prefix_len, int32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

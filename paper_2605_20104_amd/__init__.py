@@ -56,6 +56,14 @@ _SIGNATURES = {
     "graft_matrix_update": (_i32, [_vp, _vp, _vp, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _sz, _vp]),
     "graft_kv_compact": (_i32, [_vp, _vp, _i64, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _vp, _vp,
                                 _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp]),
+    "graft_kv_append": (_i32, [_vp] * 3 + [_i64] * 3 + [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _i32, _vp, _vp]
+                        + [_i32] * 7 + [_vp, _vp, _vp]),
+    "graft_kv_append_mx": (_i32, [_vp] * 3 + [_i64] * 3 + [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _i64, _i64, _vp, _i32, _vp, _vp]
+                           + [_i32] * 7 + [_vp, _vp, _vp]),
+    "graft_kv_gather_mx": (_i32, [_vp, _vp, _i64, _i32, _i64, _i64, _vp, _i32, _vp, _vp] + [_i32] * 5 + [_vp] * 4),
+    "graft_tree_attn_mx_workspace_bytes": (_sz, [_i32] * 6),
+    "graft_tree_attn_mx": (_i32, [_vp] * 3 + [_i64, _i64, _vp, _i32, _vp, _vp, _vp, _vp] + [_i32] * 6 + [_f32, _f32, _i32, _vp, _vp, _sz, _vp]),
+    "graft_kv_compact_mx": (_i32, [_vp, _vp, _i64, _i32, _i64, _i64, _vp, _i32, _vp, _vp, _vp] + [_i32] * 5 + [_vp] * 3),
 }
 EXPORTED_SYMBOLS = tuple(_SIGNATURES)
 
@@ -185,3 +193,54 @@ def graft_prune_select(parent, tokens, logq, n_nodes, chk_depth, chk_log_tau, ch
     parent, tokens, index [B,K_max], n_nodes, stage, n_ret, status [B]."""
     return _calls().prune_select(parent, tokens, logq, n_nodes, chk_depth, chk_log_tau, chk_keep, chk_ret, out,
                                 stream)
+
+
+def graft_mx_run_bytes(D: int) -> int:
+    """Bytes that a 4-bit cache spends on one page of one KV head: GRAFT_MX_RUN_BYTES.  A cache of n_pages pages is, for
+    instance, torch.zeros((n_pages, Hkv, graft_mx_run_bytes(D)), dtype=torch.uint8)."""
+    return 17 * D // 2
+
+
+def graft_kv_append(q, k, v, cos_sin, pos, k_cache, v_cache, strides, block_table, prefix_len, n_nodes,
+                    interleaved: bool = False, out=None, stream=None):
+    """Rotates the queries and keys of new tokens by their positions and writes keys and values to slots
+    prefix_len[b] + i of the paged cache.  q [B,T,Hq,D] or None, k, v [B,T,Hkv,D] float32 or bfloat16, slices of a
+    fused projection allowed; cos_sin float32 [n_pos,R] (cosines, then sines) or None; pos [B,T] from
+    graft_build_tree_mask, or None for prefix_len + i.  Returns dict(q, status [B])."""
+    return _calls().kv_append(q, k, v, cos_sin, pos, k_cache, v_cache, strides, block_table, prefix_len, n_nodes, interleaved, out, stream)
+
+
+def graft_kv_append_mx(q, k, v, cos_sin, pos, k_cache, v_cache, strides, block_table, prefix_len, n_nodes,
+                       interleaved: bool = False, out=None, stream=None):
+    """graft_kv_append into a cache of 4-bit elements (uint8 tensors; strides: dict with 'page' and 'head' in bytes)."""
+    return _calls().kv_append_mx(q, k, v, cos_sin, pos, k_cache, v_cache, strides, block_table, prefix_len, n_nodes, interleaved, out, stream)
+
+
+def graft_kv_gather_mx(k_cache, v_cache, layer_stride: int, n_layers: int, strides, block_table, start, count, T: int, Hkv: int,
+                       D: int, dtype=torch.bfloat16, out=None, stream=None):
+    """Rows start[b] .. start[b] + count[b] of a 4-bit cache as numbers.  Returns dict(k, v [n_layers,B,T,Hkv,D] of `dtype`
+    (bfloat16 or float32), status [B])."""
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("rows come back as bfloat16 or float32")
+    return _calls().kv_gather_mx(k_cache, v_cache, layer_stride, n_layers, strides, block_table, start, count, T, Hkv, D,
+                                dtype == torch.bfloat16, out, stream)
+
+
+def graft_tree_attn_mx_workspace_bytes(B: int, K_max: int, Hq: int, Hkv: int, D: int, max_pages: int) -> int:
+    return int(load_library().graft_tree_attn_mx_workspace_bytes(B, K_max, Hq, Hkv, D, max_pages))
+
+
+def graft_tree_attn_mx(q, k_cache, v_cache, strides, block_table, prefix_len, n_nodes, mask, Hkv: int, scale: float,
+                       softcap: float = 0.0, window: int = 0, pos=None, out=None, workspace=None, stream=None):
+    """Tree-masked GQA attention over a 4-bit cache, one layer.  q [B,K,Hq,D] bfloat16 on the GPU; mask from
+    graft_build_tree_mask, or None where the nodes are a chain (one token, a piece of a prompt).  softcap: scores become
+    softcap tanh(score / softcap); window: a node sees the last `window` positions (pos needed with a mask)."""
+    return _calls().tree_attn_mx(q, k_cache, v_cache, strides, block_table, prefix_len, n_nodes, mask, Hkv, scale, softcap, window, pos,
+                                out, workspace, stream)
+
+
+def graft_kv_compact_mx(k_cache, v_cache, layer_stride: int, n_layers: int, strides, block_table, prefix_len, path, accept_len,
+                        K_max: int, Hkv: int, D: int, out=None, stream=None):
+    """graft_kv_compact for a 4-bit cache.  Returns dict(new_prefix_len [B], status [B])."""
+    return _calls().kv_compact_mx(k_cache, v_cache, layer_stride, n_layers, strides, block_table, prefix_len, path, accept_len, K_max, Hkv, D,
+                                 out, stream)

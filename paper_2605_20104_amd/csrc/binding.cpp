@@ -15,6 +15,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -28,7 +29,8 @@ namespace {
     X(graft_retrieve) X(graft_build_tree_mask) X(graft_tree_attn_workspace_bytes) X(graft_tree_attn) \
     X(graft_accept_workspace_bytes) X(graft_accept) X(graft_accept_noalloc) X(graft_matrix_retrieve) \
     X(graft_matrix_update_workspace_bytes) X(graft_matrix_update) X(graft_kv_compact) X(graft_prune_select) \
-    X(graft_last_hip_error)
+    X(graft_kv_append) X(graft_kv_append_mx) X(graft_kv_gather_mx) X(graft_tree_attn_mx_workspace_bytes) X(graft_tree_attn_mx) \
+    X(graft_kv_compact_mx) X(graft_last_hip_error)
 struct Library {
 #define X(name) decltype(&::name) name = nullptr;
     GRAFT_ENTRY_POINTS(X)
@@ -189,6 +191,17 @@ public:
         T* p = static_cast<T*>(t.data_ptr());
         put(key, THPVariable_Wrap(std::move(t)));
         return p;
+    }
+    // The same, and a caller's tensor has to be of the type, the shape and on the device that a new one would be.
+    template <class T = int32_t> T* get_checked(PyObject* key, at::IntArrayRef shape, at::ScalarType type = at::kInt) {
+        if (fresh_) return get<T>(key, shape, type);
+        const Ref o(item(dict_, key));
+        const at::Tensor& t = tensor(o);
+        if (t.sizes() != shape || t.scalar_type() != type || t.device() != dev_) {
+            PyErr_Format(PyExc_ValueError, "the output %R does not have the shape, the type or the device of this call's results", key);
+            throw PythonError();
+        }
+        return ptr<T>(t);
     }
     void put(PyObject* key, PyObject* value) {                     // steals value
         const int bad = value ? PyObject_SetItem(dict_, key, value) : -1;
@@ -546,6 +559,259 @@ GRAFT_PY(py_prune_select, 10) {
     return out.release();
 }
 
+// ---- rotation and append, and the 4-bit cache ------------------------------------------------------
+[[noreturn]] void fail(PyObject* type, const char* what) {
+    PyErr_SetString(type, what);
+    throw PythonError();
+}
+
+// A whole number that fits 32 bits.
+int32_t whole(PyObject* o) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw PythonError();
+    if (v != static_cast<int32_t>(v)) fail(PyExc_OverflowError, "a size of more than 32 bits");
+    return static_cast<int32_t>(v);
+}
+
+// All tensors of a call have to be on one GPU; the call runs with that GPU as the current one.
+struct OnDevice {
+    explicit OnDevice(const at::Tensor& t) : dev(t.device()) {}
+    at::Device dev;
+    void same(const at::Tensor& t) const {
+        if (t.device() != dev) fail(PyExc_ValueError, "the tensors of a call have to be on one device");
+    }
+    void gpu() const {
+        if (!dev.is_cuda()) fail(PyExc_ValueError, "the tensors of this call have to be on the GPU");
+    }
+    // A dense array of the given type and shape; None is NULL where the call allows it.
+    template <class T> T* dense(PyObject* o, at::IntArrayRef shape, at::ScalarType type, const char* what, bool optional = false) const {
+        if (o == Py_None && optional) return nullptr;
+        const at::Tensor& t = tensor(o);
+        same(t);
+        if (t.sizes() != shape || t.scalar_type() != type) {
+            PyErr_Format(PyExc_ValueError, "%s does not have the shape or the type of this call", what);
+            throw PythonError();
+        }
+        return ptr<T>(t);
+    }
+    unsigned char* cache(PyObject* o) const {
+        const at::Tensor& t = tensor(o);
+        same(t);
+        if (t.scalar_type() != at::kByte) fail(PyExc_ValueError, "a 4-bit cache is a tensor of uint8");
+        return ptr<unsigned char>(t);
+    }
+};
+struct StridesMx { int64_t page, head; };
+StridesMx strides_mx_of(PyObject* d) { return {to_i64(item(d, s_page)), to_i64(item(d, s_head))}; }
+
+// Rows [B,T,H,D] whose tokens lie a constant number of elements apart, as a slice of a fused projection has them; that number.
+int64_t token_stride_of(const at::Tensor& t) {
+    if (t.dim() != 4) {
+        PyErr_Format(PyExc_ValueError, "expected rows of 4 dimensions, got %d", static_cast<int>(t.dim()));
+        throw PythonError();
+    }
+    const int64_t B = t.size(0), T = t.size(1), H = t.size(2), D = t.size(3);
+    const int64_t stride = T > 1 ? t.stride(1) : B > 1 ? t.stride(0) : H * D;
+    if ((D > 1 && t.stride(3) != 1) || (H > 1 && t.stride(2) != D) || (B > 1 && t.stride(0) != T * stride))
+        fail(PyExc_ValueError, "a token's heads have to be dense and tokens a constant stride apart");
+    return stride;
+}
+
+// q, k, v, cos_sin, pos, k_cache, v_cache, strides, block_table, prefix_len, n_nodes, interleaved, out, stream
+PyObject* append(PyObject* const* a, bool mx) {
+    GRAFT_KEY(q); GRAFT_KEY(status);
+    const at::Tensor &k = tensor(a[1]), &v = tensor(a[2]), &table = tensor(a[8]);
+    const OnDevice on(k);
+    const int64_t k_stride = token_stride_of(k), v_stride = token_stride_of(v);
+    const at::ScalarType type = k.scalar_type();
+    if (type != at::kFloat && type != at::kBFloat16) fail(PyExc_AssertionError, "queries, keys and values are all float32 or all bfloat16");
+    const int64_t B = k.size(0), T = k.size(1), Hkv = k.size(2), D = k.size(3);
+    auto rows_of = [&](const at::Tensor& t) {
+        on.same(t);
+        if (t.scalar_type() != type) fail(PyExc_AssertionError, "queries, keys and values are all float32 or all bfloat16");
+        if (t.size(0) != B || t.size(1) != T || t.size(3) != D) fail(PyExc_ValueError, "queries, keys and values are of different shapes");
+    };
+    rows_of(v);
+    if (v.size(2) != Hkv) fail(PyExc_ValueError, "queries, keys and values are of different shapes");
+    int64_t q_stride = 0, Hq = 0;
+    const void* q = nullptr;
+    if (a[0] != Py_None) {
+        const at::Tensor& t = tensor(a[0]);
+        q_stride = token_stride_of(t);
+        rows_of(t);
+        Hq = t.size(2);
+        q = t.data_ptr();
+    }
+    int32_t n_pos = 0, R = 0;
+    const float* angles = nullptr;
+    if (a[3] != Py_None) {
+        const at::Tensor& t = tensor(a[3]);
+        on.same(t);
+        if (t.scalar_type() != at::kFloat) fail(PyExc_ValueError, "cosines and sines are float32");
+        sizes2(t, n_pos, R);
+        angles = ptr<float>(t);
+    }
+    int32_t table_B, max_pages;
+    sizes2(table, table_B, max_pages);
+    const int32_t* pages = on.dense<int32_t>(a[8], {B, max_pages}, at::kInt, "block_table");
+    const int32_t *pl = on.dense<int32_t>(a[9], {B}, at::kInt, "prefix_len"), *n = on.dense<int32_t>(a[10], {B}, at::kInt, "n_nodes"),
+                  *pos = on.dense<int32_t>(a[4], {B, T}, at::kInt, "pos", true);
+    void *kc, *vc;
+    Strides st{0, 0, 0};
+    if (mx) {
+        kc = on.cache(a[5]);
+        vc = on.cache(a[6]);
+        const StridesMx two = strides_mx_of(a[7]);
+        st = {two.page, 0, two.head};
+    } else {
+        const at::Tensor &x = tensor(a[5]), &y = tensor(a[6]);
+        on.same(x);
+        on.same(y);
+        if (x.scalar_type() != type || y.scalar_type() != type) fail(PyExc_AssertionError, "the caches are of the rows' type");
+        kc = ptr<void>(x);
+        vc = ptr<void>(y);
+        st = strides_of(a[7]);
+    }
+    const int interleaved = PyObject_IsTrue(a[11]);
+    if (interleaved < 0) throw PythonError();
+    on.gpu();
+    const c10::DeviceGuard guard(on.dev);
+    const LaunchStream stream(a[13], on.dev);
+    Outputs out(a[12], on.dev);
+    void* q_out = q ? out.get_checked<void>(k_q, {B, T, Hq, D}, type) : nullptr;
+    int32_t* status = out.get_checked(k_status, {B});
+    const int32_t dtype = type == at::kFloat ? GRAFT_F32 : GRAFT_BF16, Bi = static_cast<int32_t>(B), Ti = static_cast<int32_t>(T);
+    const int32_t Hqi = static_cast<int32_t>(Hq), Hkvi = static_cast<int32_t>(Hkv), Di = static_cast<int32_t>(D);
+    const void *kp = k.data_ptr(), *vp = v.data_ptr();
+    void* s = stream.handle();
+    check(mx ? "graft_kv_append_mx" : "graft_kv_append", unlocked([&] {
+        return mx ? lib.graft_kv_append_mx(q, kp, vp, q_stride, k_stride, v_stride, angles, n_pos, R, interleaved, pos, kc, vc, st.page, st.head, pages,
+                                           max_pages, pl, n, Bi, Ti, Hqi, Hkvi, Di, GRAFT_PAGE_SIZE, dtype, q_out, status, s)
+                  : lib.graft_kv_append(q, kp, vp, q_stride, k_stride, v_stride, angles, n_pos, R, interleaved, pos, kc, vc, st.page, st.token, st.head,
+                                        pages, max_pages, pl, n, Bi, Ti, Hqi, Hkvi, Di, GRAFT_PAGE_SIZE, dtype, q_out, status, s);
+    }));
+    return out.release();
+}
+GRAFT_PY(py_kv_append, 14) { return append(a, false); }
+GRAFT_PY(py_kv_append_mx, 14) { return append(a, true); }
+
+// k_cache, v_cache, layer_stride, n_layers, strides, block_table, start, count, T, Hkv, D, bf16, out, stream
+GRAFT_PY(py_kv_gather_mx, 14) {
+    GRAFT_KEY(k); GRAFT_KEY(v); GRAFT_KEY(status);
+    const at::Tensor& table = tensor(a[5]);
+    const OnDevice on(table);
+    const unsigned char *kc = on.cache(a[0]), *vc = on.cache(a[1]);
+    const int64_t layer_stride = to_i64(a[2]);
+    const int32_t n_layers = whole(a[3]), T = whole(a[8]), Hkv = whole(a[9]), D = whole(a[10]);
+    const StridesMx st = strides_mx_of(a[4]);
+    int32_t B, max_pages;
+    sizes2(table, B, max_pages);
+    const int32_t* pages = on.dense<int32_t>(a[5], {B, max_pages}, at::kInt, "block_table");
+    const int32_t *start = on.dense<int32_t>(a[6], {B}, at::kInt, "start", true), *count = on.dense<int32_t>(a[7], {B}, at::kInt, "count");
+    const int bf16 = PyObject_IsTrue(a[11]);
+    if (bf16 < 0) throw PythonError();
+    if (n_layers < 1 || T < 1 || Hkv < 1 || D < 1) fail(PyExc_ValueError, "n_layers, T, Hkv and D are positive");
+    on.gpu();
+    const c10::DeviceGuard guard(on.dev);
+    const LaunchStream stream(a[13], on.dev);
+    Outputs out(a[12], on.dev);
+    const at::ScalarType type = bf16 ? at::kBFloat16 : at::kFloat;
+    void* ko = out.get_checked<void>(k_k, {n_layers, B, T, Hkv, D}, type);
+    void* vo = out.get_checked<void>(k_v, {n_layers, B, T, Hkv, D}, type);
+    int32_t* status = out.get_checked(k_status, {B});
+    void* s = stream.handle();
+    check("graft_kv_gather_mx", unlocked([&] {
+        return lib.graft_kv_gather_mx(kc, vc, layer_stride, n_layers, st.page, st.head, pages, max_pages, start, count, B, T, Hkv, D,
+                                      bf16 ? GRAFT_BF16 : GRAFT_F32, ko, vo, status, s);
+    }));
+    return out.release();
+}
+
+// q, k_cache, v_cache, strides, block_table, prefix_len, n_nodes, mask, Hkv, scale, softcap, window, pos, out, workspace, stream
+GRAFT_PY(py_tree_attn_mx, 16) {
+    const at::Tensor &q = tensor(a[0]), &table = tensor(a[4]);
+    const OnDevice on(q);
+    if (q.dim() != 4) {
+        PyErr_Format(PyExc_ValueError, "expected a query tensor of 4 dimensions, got %d", static_cast<int>(q.dim()));
+        throw PythonError();
+    }
+    if (q.scalar_type() != at::kBFloat16) fail(PyExc_AssertionError, "queries over a 4-bit cache are bfloat16");
+    const int32_t B = size_at(q, 0), K = size_at(q, 1), Hq = size_at(q, 2), D = size_at(q, 3), Hkv = whole(a[8]), window = whole(a[11]);
+    const unsigned char *kc = on.cache(a[1]), *vc = on.cache(a[2]);
+    const StridesMx st = strides_mx_of(a[3]);
+    int32_t table_B, max_pages;
+    sizes2(table, table_B, max_pages);
+    const int32_t* pages = on.dense<int32_t>(a[4], {B, max_pages}, at::kInt, "block_table");
+    const int32_t *pl = on.dense<int32_t>(a[5], {B}, at::kInt, "prefix_len"), *n = on.dense<int32_t>(a[6], {B}, at::kInt, "n_nodes"),
+                  *pos = on.dense<int32_t>(a[12], {B, K}, at::kInt, "pos", true);
+    const uint64_t* mask = on.dense<uint64_t>(a[7], {B, K, GRAFT_MASK_WORDS}, at::kLong, "mask", true);
+    const double scale = PyFloat_AsDouble(a[9]);
+    if (scale == -1.0 && PyErr_Occurred()) throw PythonError();
+    const double cap = PyFloat_AsDouble(a[10]);
+    if (cap == -1.0 && PyErr_Occurred()) throw PythonError();
+    const void* qp = ptr<void>(q);
+    on.gpu();
+    const c10::DeviceGuard guard(on.dev);
+    const LaunchStream stream(a[15], on.dev);
+    at::Tensor new_out, new_ws;
+    void* out;
+    if (a[13] == Py_None) {
+        new_out = empty(q.sizes(), at::kBFloat16, on.dev);
+        out = new_out.data_ptr();
+    } else out = on.dense<void>(a[13], q.sizes(), at::kBFloat16, "out");
+    void* ws = nullptr;
+    size_t ws_bytes = 0;
+    if (a[14] == Py_None) {
+        ws_bytes = lib.graft_tree_attn_mx_workspace_bytes(B, K, Hq, Hkv, D, max_pages);
+        if (ws_bytes > 0) {
+            new_ws = stream.scratch(ws_bytes);
+            ws = new_ws.data_ptr();
+        }
+    } else {
+        const at::Tensor& w = tensor(a[14]);
+        on.same(w);
+        ws = ptr<void>(w);
+        ws_bytes = w.nbytes();
+    }
+    void* s = stream.handle();
+    check("graft_tree_attn_mx", unlocked([&] {
+        return lib.graft_tree_attn_mx(qp, kc, vc, st.page, st.head, pages, max_pages, pl, n, mask, pos, B, K, Hq, Hkv, D, GRAFT_PAGE_SIZE,
+                                      static_cast<float>(scale), static_cast<float>(cap), window, out, ws, ws_bytes, s);
+    }));
+    if (new_out.defined()) return THPVariable_Wrap(std::move(new_out));
+    Py_INCREF(a[13]);
+    return a[13];
+}
+
+// k_cache, v_cache, layer_stride, n_layers, strides, block_table, prefix_len, path, accept_len, K_max, Hkv, D, out, stream
+GRAFT_PY(py_kv_compact_mx, 14) {
+    GRAFT_KEY(new_prefix_len); GRAFT_KEY(status);
+    const at::Tensor &table = tensor(a[5]), &path = tensor(a[7]);
+    const OnDevice on(path);
+    int32_t B, width, table_B, max_pages;
+    sizes2(path, B, width);
+    sizes2(table, table_B, max_pages);
+    unsigned char *kc = on.cache(a[0]), *vc = on.cache(a[1]);
+    const int64_t layer_stride = to_i64(a[2]);
+    const int32_t n_layers = whole(a[3]), K = whole(a[9]), Hkv = whole(a[10]), D = whole(a[11]);
+    const StridesMx st = strides_mx_of(a[4]);
+    const int32_t* pages = on.dense<int32_t>(a[5], {B, max_pages}, at::kInt, "block_table");
+    const int32_t *pl = on.dense<int32_t>(a[6], {B}, at::kInt, "prefix_len"), *pp = on.dense<int32_t>(a[7], {B, width}, at::kInt, "path"),
+                  *al = on.dense<int32_t>(a[8], {B}, at::kInt, "accept_len");
+    on.gpu();
+    const c10::DeviceGuard guard(on.dev);
+    const LaunchStream stream(a[13], on.dev);
+    Outputs out(a[12], on.dev);
+    int32_t* new_len = out.get_checked(k_new_prefix_len, {B});
+    int32_t* status = out.get_checked(k_status, {B});
+    void* s = stream.handle();
+    check("graft_kv_compact_mx", unlocked([&] {
+        return lib.graft_kv_compact_mx(kc, vc, layer_stride, n_layers, st.page, st.head, pages, max_pages, pl, pp, al, B, width - 1, K, Hkv, D,
+                                       new_len, status, s);
+    }));
+    return out.release();
+}
+
 // path of the library, GraftError
 PyObject* py_bind(PyObject*, PyObject* args) {
     const char* path;
@@ -571,7 +837,8 @@ PyMethodDef methods[] = {
     {"bind", py_bind, METH_VARARGS, "bind(path, error_class): resolve the library's entry points"},
     GRAFT_METHOD(retrieve), GRAFT_METHOD(build_tree_mask), GRAFT_METHOD(tree_attn), GRAFT_METHOD(accept),
     GRAFT_METHOD(accept_noalloc), GRAFT_METHOD(matrix_retrieve), GRAFT_METHOD(matrix_update), GRAFT_METHOD(kv_compact),
-    GRAFT_METHOD(prune_select), {nullptr, nullptr, 0, nullptr}};
+    GRAFT_METHOD(prune_select), GRAFT_METHOD(kv_append), GRAFT_METHOD(kv_append_mx), GRAFT_METHOD(kv_gather_mx),
+    GRAFT_METHOD(tree_attn_mx), GRAFT_METHOD(kv_compact_mx), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "Marshalling of the graft_* calls.", -1, methods,
                           nullptr, nullptr, nullptr, nullptr};
 
