@@ -507,7 +507,8 @@ int32_t graft_kv_gather_mx(const void* k_cache, const void* v_cache, int64_t lay
  * run at the same time need one each.  It depends on the current device, as graft_tree_attn_workspace_bytes does.
  *
  * Requires D in {64,128}, Hq % Hkv == 0, Hq/Hkv <= 16, 1 <= K_max <= GRAFT_MAX_NODES, 1 <= max_pages <= 262144,
- * window >= 0, softcap >= 0 and finite, scale finite, q and out 16-byte aligned.
+ * B <= 65535, B * Hkv <= 2^18, page_stride < 2^32 (bytes; the cache itself may be larger), window >= 0, softcap >= 0 and finite, scale
+ * finite, q and out 16-byte aligned.
  */
 size_t graft_tree_attn_mx_workspace_bytes(int32_t B, int32_t K_max, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_pages);
 

@@ -1,8 +1,7 @@
 // graft_tree_attn_mx: tree-masked attention over a cache of 4-bit elements (mx.h).
 //
 // For a row (node and query head) and its tokens t: x_t = scale q.k_t, or c tanh(x_t / c) with a cap c; out = sum p_t v_t / sum p_t,
-// p_t = exp(x_t - m), in one pass over the keys with a running maximum m (kept where it is until a score exceeds it by 2^8:
-// probabilities and sums are the same floating-point numbers up to a power of two).
+// p_t = exp(x_t - m), in one pass over the keys with a running maximum m.
 //
 // Scores: 4-bit keys enter the matrix cores as they are in memory (v_mfma_scale_f32_16x16x128_f8f6f4, 16 tokens x 16 rows x 128
 // elements).  At the rate of 4 and 6 bits, twice that of 8, a query takes three e2m3 numbers of 6 bits: its block of 32 elements is scaled to
@@ -10,7 +9,7 @@
 // element is left out, less than the rounding of probabilities below makes of a score.  48 cycles, as bf16 operands take 64, and no
 // conversion of keys.
 // Values: scales are per token, the matrix cores' per 32 summands, so values are converted to bfloat16 (exact: one bit of mantissa and a
-// power of two), probabilities are rounded to bfloat16 (2^-9 each, the choice of the kernels over bfloat16 caches), sums are float32.
+// power of two), probabilities are rounded to bfloat16 (2^-8 of each, the choice of the kernels over bfloat16 caches), sums are float32.
 // Scores come out of the matrix cores as D[token][row]: lane l has row l % 16, tokens 4 (l / 16) .. + 4 of each page; that is the layout in
 // which the second product takes probabilities (with 8 tokens a lane, 4 from each of two pages), so nothing crosses lanes.
 #include "mx.h"
@@ -28,20 +27,22 @@ typedef __bf16 Bf2 __attribute__((ext_vector_type(2)));
 typedef __bf16 Bf8 __attribute__((ext_vector_type(8)));
 
 constexpr int TM_WAVES = 4, TM_THREADS = 64 * TM_WAVES;
+constexpr int TM_MAX_SPLITS = 64;
 constexpr float TM_LOW = -3.402823466e38f;         // no score yet: below or equal to every finite score
-constexpr float TM_SLACK = 8.0f;                   // powers of two by which a score may exceed the running maximum
+constexpr float TM_MOST = 4096.0f;                 // sum of a lane's probabilities of a tile from which on the maximum is raised
 
 struct AttnMxParams {
     const unsigned short* q;
     const unsigned char *k_cache, *v_cache;
-    const int32_t *block_table, *pos;
+    const int32_t* pos;
     const u64* mask;
     unsigned short* out;
     float *partial, *stat;                         // [B,Hkv,S,rows] x D and x 2, where keys are split over workgroups
-    int64_t page_stride, head_stride;              // bytes
-    float factor, cap_in, cap_out;                 // of a raw score: to powers of two; with a cap 2 log2(e) / c, and c log2(e)
-    int32_t sign;                                  // of the scale
-    int32_t K, Hkv, G, max_pages, window, splits, row_tiles, items;
+    int64_t head_stride;                           // bytes
+    unsigned page_stride;
+    float factor, cap;                             // of queries, so that scores are powers of two, or with a cap c 2 x / c is one; c log2(e)
+    unsigned per_group;                            // rows to nodes: 2^16 / G, rounded up
+    int32_t K, Hkv, G, max_pages, window, splits, row_tiles, waves, items;       // (waves: of a workgroup, that have rows)
 };
 
 // One row's 32 elements of a lane in three parts of 6 bits, and the parts' scale bytes.
@@ -49,28 +50,26 @@ struct Query {
     UInt6 part[3];
     int bytes;
 };
-__device__ __forceinline__ Query split_query(const float* x) {
-    unsigned top = 0;
+__device__ __forceinline__ Query split_query(const UInt4 (&raw)[4], float factor) {        // 32 elements of bfloat16, times the factor
+    typedef unsigned short Short2 __attribute__((ext_vector_type(2)));
+    Short2 most = {0, 0};
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-        const unsigned u = __float_as_uint(x[j]) & 0x7FFFFFFFu;
-        top = u > top ? u : top;
-    }
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(Short2, raw[i][j] & 0x7FFF7FFFu));
+    const unsigned top = __float_as_uint(__uint_as_float(static_cast<unsigned>(most[0] > most[1] ? most[0] : most[1]) << 16) * factor) & 0x7FFFFFFFu;
     int byte = static_cast<int>((top + 0x0FFFFFu) >> 23) - 2;      // (largest element within (3.75, 7.5] of it)
     byte = byte < 12 ? 12 : byte > 252 ? 252 : byte;
     Query q;
-    float rest[32];
+    Float16 even, odd;                             // elements 2 j, 2 j + 1
 #pragma unroll
-    for (int j = 0; j < 32; ++j) rest[j] = x[j];
+    for (int j = 0; j < 16; ++j) {
+        even[j] = __uint_as_float(raw[j / 4][j % 4] << 16) * factor;
+        odd[j] = __uint_as_float(raw[j / 4][j % 4] & 0xFFFF0000u) * factor;
+    }
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-        const float scale = mx_scale(byte - (i == 0 ? 0 : i == 1 ? 4 : 9));
-        Float16 even, odd;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            even[j] = rest[2 * j];
-            odd[j] = rest[2 * j + 1];
-        }
+        float scale = mx_scale(byte - (i == 0 ? 0 : i == 1 ? 4 : 9));
         // These two conversions take several cycles and write their first results before they read their last operands, which the
         // compiler does not know: it placed the scale in a register of the result, and the third part of a query came out wrong.
         // The statements behind them keep the operands' registers in use until the results are there.
@@ -80,7 +79,10 @@ __device__ __forceinline__ Query split_query(const float* x) {
             Float32 held = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q.part[i], scale);
             asm volatile("" : "+v"(held) : "v"(q.part[i]), "v"(scale));
 #pragma unroll
-            for (int j = 0; j < 32; ++j) rest[j] -= held[j];
+            for (int j = 0; j < 16; ++j) {
+                even[j] -= held[2 * j];
+                odd[j] -= held[2 * j + 1];
+            }
         }
     }
     q.bytes = byte | (byte - 4) << 8 | (byte - 9) << 16;
@@ -88,267 +90,518 @@ __device__ __forceinline__ Query split_query(const float* x) {
     return q;
 }
 
-// Keys and values of NP pages as they are in memory, this lane's 16 bytes (values: 8 with D = 64) and scale bytes.
-template <int D, int NP> struct Pages {
-    using V = std::conditional_t<D == 128, UInt4, UInt2>;
-    UInt4 k[NP];
-    V v[NP];
-    unsigned k_scale[NP], v_scale[NP];
+// What a workgroup knows of its sequence.
+struct Sequence {
+    int P, n, L, rows, all_rows;                   // prefix, nodes, their sum; rows (node, head of the group) that are there, and slots
+    int first_page, end_page, all_see;             // pages that some node sees; the first token from which on every node sees all of the prefix
+    bool deep;                                     // some node does not see an ancestor any more
+    const int32_t *table, *pos;
+    const u64* mask;
+    int64_t out;                                   // element of the sequence's first row
 };
 
+__device__ __forceinline__ Sequence sequence_of(int b, int P, int n, const int32_t* block_table, const AttnMxParams& p, int D) {
+    Sequence q;
+    if (P < 0 || n < 0 || n > p.K || static_cast<int64_t>(P) + n > static_cast<int64_t>(p.max_pages) * GRAFT_PAGE_SIZE) n = 0;
+    q.P = P;
+    q.n = n;
+    q.L = P + n;
+    q.rows = n * p.G;
+    q.all_rows = p.K * p.G;
+    q.table = block_table + static_cast<int64_t>(b) * p.max_pages;
+    q.pos = p.pos ? p.pos + static_cast<int64_t>(b) * p.K : nullptr;
+    q.mask = p.mask ? p.mask + static_cast<int64_t>(b) * p.K * GRAFT_MASK_WORDS : nullptr;
+    q.out = static_cast<int64_t>(b) * p.K * p.Hkv * p.G * D;
+    q.first_page = 0;
+    q.all_see = 0;
+    q.deep = false;
+    q.end_page = (q.L + GRAFT_PAGE_SIZE - 1) / GRAFT_PAGE_SIZE;
+    return q;
+}
+
+// With a window: the pages in front of every node's are left out.
+__device__ __forceinline__ void look_back(Sequence& q, int window, int lane) {
+    int low = 0x7FFFFFFF, high = -0x7FFFFFFF;
+    for (int i = lane; i < q.n; i += 64) {
+        const int at = q.pos ? q.pos[i] : q.P + i;
+        low = at < low ? at : low;
+        high = at > high ? at : high;
+    }
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) {
+        const int l2 = __shfl_xor(low, s), h2 = __shfl_xor(high, s);
+        low = l2 < low ? l2 : low;
+        high = h2 > high ? h2 : high;
+    }
+    const int64_t from = static_cast<int64_t>(low) - window + 1, all = static_cast<int64_t>(high) - window + 1;
+    q.first_page = __builtin_amdgcn_readfirstlane(static_cast<int>(from < 0 ? 0 : from > q.P ? q.P : from) / GRAFT_PAGE_SIZE);
+    q.all_see = __builtin_amdgcn_readfirstlane(static_cast<int>(all < 0 ? 0 : all > q.P ? q.P : all));
+    q.deep = __builtin_amdgcn_readfirstlane(static_cast<int64_t>(high) - low >= window) != 0;
+}
+
+// row / G: rows are fewer than 2^11 and G is 16 at most, so the product is less than 1 / 32 above the quotient's 1 / G steps.
+static_assert(GRAFT_MAX_NODES * 16 <= 2048, "the division of rows by heads");
+__device__ __forceinline__ int node_of(const AttnMxParams& p, int row) { return static_cast<int>((static_cast<unsigned>(row) * p.per_group) >> 16); }
+
+// Element of a row of KV head g in q and out.
+__device__ __forceinline__ int64_t row_at(const Sequence& q, const AttnMxParams& p, int g, int row, int D) {
+    const int node = node_of(p, row);
+    return q.out + (static_cast<int64_t>(node) * p.Hkv * p.G + g * p.G + (row - node * p.G)) * D;
+}
+
+// A split's units (tiles or stages of `tokens` tokens): those in front of `whole` and from `whole_end` on (where windows begin, and at the tree) are not
+// seen whole by every node.  They are taken from `whole` on, around the end to the first ones: sums over keys have no order, and so one
+// loop without masks and one with them see to all.
+struct Units {
+    int first, count, whole, whole_end;            // first unit of all; the rest counted from it
+    __device__ __forceinline__ Units(const Sequence& q, int tokens, int split, int splits) {
+        const int per = tokens / GRAFT_PAGE_SIZE, units = (q.end_page - q.first_page + per - 1) / per, base = q.first_page * GRAFT_PAGE_SIZE;
+        // (2^18 units, 2^8 splits at most)
+        first = static_cast<int>(static_cast<unsigned>(units) * static_cast<unsigned>(split) / static_cast<unsigned>(splits));
+        count = static_cast<int>(static_cast<unsigned>(units) * static_cast<unsigned>(split + 1) / static_cast<unsigned>(splits)) - first;
+        whole = min(max((max(q.all_see - base, 0) + tokens - 1) / tokens - first, 0), count);
+        whole_end = max(min(max(q.P - base, 0) / tokens - first, count), whole);
+    }
+    __device__ __forceinline__ int end() const { return whole + count; }
+    __device__ __forceinline__ int unit(int i) const { return i < count ? i : i - count; }
+};
+
+// The page numbers of the units: lane j of `here` has that of page 64 block + j (counted from the first unit's), of `next` that of the block behind it,
+// on its way since the last change of blocks.  A number is read across lanes, without a trip to memory in front of the
+// loads that it addresses.
+struct PageIds {
+    const int32_t* table;
+    int last, lane, block, here, next;             // the last page there is; pages past it are taken for it
+    __device__ __forceinline__ PageIds(const Sequence& q, int first_page, int lane_) : table(q.table + first_page), last(q.end_page - 1 - first_page), lane(lane_), block(0) {
+        here = load(0);
+        next = load(1);
+    }
+    __device__ __forceinline__ int load(int b) const { return table[min(64 * b + lane, last)]; }
+    __device__ __forceinline__ void seek(int page) {                // uniform
+        const int b = page >> 6;
+        if (b == block) return;
+        here = b == block + 1 ? next : load(b);
+        next = load(b + 1);
+        block = b;
+    }
+    __device__ __forceinline__ u64 offset(int page, unsigned stride) const {
+        return static_cast<u64>(static_cast<unsigned>(__builtin_amdgcn_readlane(here, page & 63))) * stride;
+    }
+};
+
+// Zeros for a tile of rows of padding nodes.
+__device__ __forceinline__ void zero_rows(const Sequence& q, const AttnMxParams& p, int g, int row0, int count, int D) {
+    for (int i = threadIdx.x; i < count * (D / 8); i += blockDim.x) {
+        const int row = row0 + i / (D / 8);
+        if (row < q.all_rows) *reinterpret_cast<UInt4*>(p.out + row_at(q, p, g, row, D) + i % (D / 8) * 8) = UInt4{0, 0, 0, 0};
+    }
+}
+
+// 32 elements of a row's query from `from` on; zeros past the row's end.  Rows that are not there get some row's: what comes of it stays
+// in their column of the products.
+template <int D> __device__ __forceinline__ Query load_query(const Sequence& q, const AttnMxParams& p, int g, int row, int from) {
+    const bool there = from < D;
+    const UInt4* src = reinterpret_cast<const UInt4*>(p.q + row_at(q, p, g, row < q.rows ? row : 0, D) + (there ? from : 0));
+    UInt4 raw[4];
+    const unsigned keep = there ? ~0u : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = src[i] & keep;
+    return split_query(raw, p.factor);
+}
+
+// Where a lane's bytes of a run are.
+template <int D> struct LaneAt {
+    unsigned k, k_scale, v, v_scale;
+    __device__ __forceinline__ explicit LaneAt(int lane) {
+        const int row16 = lane & 15, quad = lane >> 4, block = quad & (D / 32 - 1);   // (D = 64: lanes past the row's end have zeros of the query)
+        k = row16 * (D / 2) + block * 16;
+        k_scale = mx_scale_at<D>(row16, block);
+        v = lane * (D / 8);
+        v_scale = mx_scale_at<D>(quad * 4, row16 * (D / 16) / 32);
+    }
+};
+
+// A run as a buffer: one base for all lanes, 32 bits of offset in each, and nothing outside it is read.
+template <int D> __device__ __forceinline__ __amdgpu_buffer_rsrc_t run_of(const unsigned char* base) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, mx_run_bytes(D), 0x00020000);
+}
+
+// A lane's bytes of a page's values.
+template <int D> struct ValuePage {
+    using V = std::conditional_t<D == 128, UInt4, UInt2>;
+    V four;
+    unsigned scale;
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t run, unsigned at, unsigned scale_at) {
+        if constexpr (D == 128) four = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(run, at, 0, 0));
+        else four = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(run, at, 0, 0));
+        scale = __builtin_amdgcn_raw_buffer_load_b32(run, scale_at, 0, 0);
+    }
+    // Values of tokens behind the last one and values that are no numbers become small ones, which a probability of 0 takes out.
+    __device__ __forceinline__ void keep_numbers(int first_token, int L) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (first_token + r >= L || ((scale >> (8 * r)) & 255u) == MX_NAN) scale = (scale & ~(255u << (8 * r))) | 2u << (8 * r);
+    }
+};
+
+// Bit r: the value of token 4 quad + r of a page is no number in any of its blocks, which the 16 lanes of a quad hold between them.
+__device__ __forceinline__ unsigned no_numbers(unsigned scale, int quad) {
+    unsigned any = 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const u64 lanes = __builtin_amdgcn_ballot_w64(((scale >> (8 * r)) & 255u) == MX_NAN);
+        any |= (lanes >> (16 * quad) & 0xFFFFull) != 0 ? 1u << r : 0u;
+    }
+    return any;
+}
+
+// Adds one part's products to the raw scores of 16 tokens and 16 rows; the keys' scale is byte BYTE of `scale`.
+template <int BYTE, int PART> __device__ __forceinline__ Float4 add_scores(UInt4 key, unsigned scale, const Query& q, Float4 s) {
+    const UInt6 u = q.part[PART];
+    const Int8 a = {static_cast<int>(key[0]), static_cast<int>(key[1]), static_cast<int>(key[2]), static_cast<int>(key[3]), 0, 0, 0, 0};
+    const Int8 b = {static_cast<int>(u[0]), static_cast<int>(u[1]), static_cast<int>(u[2]), static_cast<int>(u[3]), static_cast<int>(u[4]), static_cast<int>(u[5]), 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, s, 4, 2, BYTE, scale, PART, q.bytes);
+}
+// The scores of four pages, less the rows' maxima so far (`start`), the small parts of the queries first; pages in turn, so that no product
+// waits for the one in front.  The keys' scales: a register for each page, or a byte of one.
+__device__ __forceinline__ void scores(const UInt4 (&key)[4], const unsigned (&scale)[4], const Query& q, float start, Float4 (&s)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = add_scores<0, 2>(key[i], scale[i], q, Float4{start, start, start, start});
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = add_scores<0, 1>(key[i], scale[i], q, s[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = add_scores<0, 0>(key[i], scale[i], q, s[i]);
+}
+template <int PART> __device__ __forceinline__ void scores_of_part(const UInt4 (&key)[4], unsigned scales, const Query& q, Float4 (&s)[4]) {
+    s[0] = add_scores<0, PART>(key[0], scales, q, s[0]);
+    s[1] = add_scores<1, PART>(key[1], scales, q, s[1]);
+    s[2] = add_scores<2, PART>(key[2], scales, q, s[2]);
+    s[3] = add_scores<3, PART>(key[3], scales, q, s[3]);
+}
+__device__ __forceinline__ void scores(const UInt4 (&key)[4], unsigned scales, const Query& q, float start, Float4 (&s)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = Float4{start, start, start, start};
+    scores_of_part<2>(key, scales, q, s);
+    scores_of_part<1>(key, scales, q, s);
+    scores_of_part<0>(key, scales, q, s);
+}
+
+// What a row sees: tree slots (those past the last node taken out), and prefix tokens behind `last`.
+struct Sight {
+    u64 word[2];
+    int last;
+};
+__device__ __forceinline__ Sight sight_of(const Sequence& q, int window, int node, int lane) {
+    auto low = [](int count) { return count >= 64 ? ~0ull : count <= 0 ? 0ull : (1ull << count) - 1; };
+    Sight x{{low(node + 1), low(node + 1 - 64)}, -1};              // (a chain)
+    if (q.mask) {
+        x.word[0] = q.mask[node * GRAFT_MASK_WORDS];
+        x.word[1] = q.mask[node * GRAFT_MASK_WORDS + 1];
+    }
+    x.word[0] &= low(q.n);
+    x.word[1] &= low(q.n - 64);
+    if (window > 0) {                              // uniform
+        const int64_t last = (q.pos ? q.pos[node] : q.P + node) - static_cast<int64_t>(window);
+        x.last = static_cast<int>(last < -1 ? -1 : last > q.P ? q.P : last);
+        if (q.deep) {
+            const int at[2] = {q.pos ? q.pos[min(lane, q.n - 1)] : q.P + lane, q.pos ? q.pos[min(lane + 64, q.n - 1)] : q.P + lane + 64};
+            for (int j = 0; j < q.n; ++j) {
+                const int place = __builtin_amdgcn_readlane(j < 64 ? at[0] : at[1], j & 63);
+                const u64 bit = place > last ? 0ull : 1ull << (j & 63);
+                if (j < 64) x.word[0] &= ~bit;
+                else x.word[1] &= ~bit;
+            }
+        }
+    }
+    return x;
+}
+
+__device__ __forceinline__ bool sees(const Sequence& q, const Sight& sight, int token) {
+    const int j = token - q.P;
+    const unsigned slot = static_cast<unsigned>((j & 64 ? sight.word[1] : sight.word[0]) >> (j & 63)) & 1u;
+    return j < 0 ? token > sight.last : j < GRAFT_MAX_NODES && slot != 0;
+}
+
+// Where a tile of NP pages from token `first` on is not seen whole by every node: what this lane's row does not see becomes -inf, what it sees and
+// has a value that is no number becomes NaN (no_number: bit 4 i + r).
+template <int NP>
+__device__ __forceinline__ void mask_scores(Float4 (&s)[NP], const Sequence& q, const Sight& sight, int first, int quad, unsigned no_number) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float x = (no_number >> (4 * i + r) & 1) ? __builtin_nanf("") : s[i][r];
+            s[i][r] = sees(q, sight, first + i * GRAFT_PAGE_SIZE + quad * 4 + r) ? x : -__builtin_inff();
+        }
+}
+
+// With a cap c the products are y = 2 log2(e) x / c: c tanh(x / c) = c - 2 c / (2^y + 1), in powers of two, less the row's maximum so far.
+template <int NP> __device__ __forceinline__ void cap_scores(Float4 (&s)[NP], float cap, float start) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            s[i][r] = __builtin_fmaf(__builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[i][r]) + 1.0f), -2.0f * cap, cap) + start;
+}
+
+// A row block's softmax: the maximum `top` that scores are taken less of (TM_LOW as long as the row has seen nothing; common to its four
+// lanes), this lane's part `sum` of the row's sum, and the weighted sum of values.
+template <int TILES> struct Softmax {
+    float top, sum;
+    Float4 acc[TILES];
+    __device__ __forceinline__ void clear() {
+        top = TM_LOW;
+        sum = 0.0f;
+#pragma unroll
+        for (int m = 0; m < TILES; ++m) acc[m] = Float4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ float start() const { return top == TM_LOW ? 0.0f : -top; }
+    // A new maximum, of what the row has seen and these scores; by how much it rose.
+    template <int NP> __device__ __forceinline__ float raise(Float4 (&s)[NP]) {
+        float most = __builtin_fmaxf(s[0][0], s[0][1]);
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int r = i == 0 ? 2 : 0; r < 4; r += 2) most = __builtin_fmaxf(__builtin_fmaxf(most, s[i][r]), s[i][r + 1]);
+        most = rows_max_f32(most);
+        const bool fresh = top == TM_LOW;
+        float up = fresh ? most : __builtin_fmaxf(most, 0.0f);
+        if (up == -__builtin_inff()) up = 0.0f;    // (nothing seen yet, and nothing here)
+        else top = (fresh ? 0.0f : top) + up;
+        const float shrink = fresh ? 1.0f : __builtin_amdgcn_exp2f(-up);
+        sum *= shrink;
+#pragma unroll
+        for (int m = 0; m < TILES; ++m) acc[m] *= shrink;
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[i][r] -= up;
+        return up;
+    }
+};
+template <int NP> __device__ __forceinline__ float powers(const Float4 (&s)[NP], Float4 (&x)[NP]) {        // and their sum
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            x[i][r] = __builtin_amdgcn_exp2f(s[i][r]);
+            sum[r & 1] += x[i][r];
+        }
+    return sum[0] + sum[1];
+}
+template <int NP> __device__ __forceinline__ void to_operand(const Float4 (&x)[NP], Bf8 (&prob)[NP / 2]) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) prob[i / 2][(i & 1) * 4 + r] = static_cast<__bf16>(x[i][r]);
+}
+// Scores to probabilities.  With ALWAYS, or `first`, the maxima are brought up to date first.  Else they are left as they are as long as the
+// probabilities add up to less than TM_MOST in every lane: they and their sums are floating-point numbers, the same up to a power of
+// two.  (So the common case takes no maximum: an exponential, half a conversion and an addition a score.)
+template <int MB, int NP, bool ALWAYS, int TILES>
+__device__ __forceinline__ void to_probabilities(Float4 (&s)[MB][NP], bool first, Softmax<TILES> (&soft)[MB], Bf8 (&prob)[MB][NP / 2]) {
+    Float4 x[MB][NP];
+    float sum[MB];
+    if constexpr (ALWAYS) {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            soft[mb].raise(s[mb]);
+            sum[mb] = powers<NP>(s[mb], x[mb]);
+        }
+    } else {
+        bool over = first;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            sum[mb] = powers<NP>(s[mb], x[mb]);
+            over = over || sum[mb] > TM_MOST;
+        }
+        if (__builtin_amdgcn_ballot_w64(over) != 0) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                soft[mb].raise(s[mb]);
+                sum[mb] = powers<NP>(s[mb], x[mb]);
+            }
+        }
+    }
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        soft[mb].sum += sum[mb];
+        to_operand<NP>(x[mb], prob[mb]);
+    }
+}
+
+// Part PAIR of a page's values as halves of operands (4 of their 8 tokens a lane): elements 2 PAIR and 2 PAIR + 1 of the lane's part of its tokens.
+template <int D, int PAIR> __device__ __forceinline__ void value_pair(const ValuePage<D>& v, const float (&scale)[4], UInt2 (&two)[2]) {
+    unsigned c[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        if constexpr (D == 128) c[r] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.four[r], scale[r], PAIR));
+        else if (r & 1) c[r] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.four[r / 2], scale[r], 2 + PAIR));
+        else c[r] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.four[r / 2], scale[r], PAIR));
+    }
+    two[0] = UInt2{__builtin_amdgcn_perm(c[1], c[0], 0x05040100), __builtin_amdgcn_perm(c[3], c[2], 0x05040100)};
+    two[1] = UInt2{__builtin_amdgcn_perm(c[1], c[0], 0x07060302), __builtin_amdgcn_perm(c[3], c[2], 0x07060302)};
+}
+template <int D> __device__ __forceinline__ void value_scales(const ValuePage<D>& v, float (&scale)[4]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) scale[r] = mx_scale((v.scale >> (8 * r)) & 255u);
+}
+
+template <class F, int... I> __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F> __device__ __forceinline__ void each(F&& f) { each_of(std::make_integer_sequence<int, N>{}, f); }
+
+// All of them: `put` gets element 0, 1, ..
+template <int D, class Put> __device__ __forceinline__ void value_operands(const ValuePage<D>& v, Put&& put) {
+    float scale[4];
+    value_scales<D>(v, scale);
+    each<D / 32>([&](auto pair) {
+        UInt2 two[2];
+        value_pair<D, decltype(pair)::value>(v, scale, two);
+        put(2 * decltype(pair)::value, two[0]);
+        put(2 * decltype(pair)::value + 1, two[1]);
+    });
+}
+
+// N neighbouring elements of a row from `d` on: the result, or with the keys split the sums.
+template <int D, int N>
+__device__ __forceinline__ void store_part(const Sequence& q, const AttnMxParams& p, int64_t out_at, int64_t item, int row, int d, const float (&o)[N], float total) {
+    if (row >= q.all_rows) return;
+    if (p.splits == 1) {
+        const bool there = row < q.rows;
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        unsigned packed[N / 2];
+#pragma unroll
+        for (int m = 0; m < N; m += 2) {
+            const Bf2 two = {static_cast<__bf16>(there ? o[m] * inv : 0.0f), static_cast<__bf16>(there ? o[m + 1] * inv : 0.0f)};
+            packed[m / 2] = __builtin_bit_cast(unsigned, two);
+        }
+        unsigned short* out = p.out + out_at + d;
+        if constexpr (N % 8 == 0) {
+#pragma unroll
+            for (int m = 0; m < N / 8; ++m) reinterpret_cast<UInt4*>(out)[m] = UInt4{packed[4 * m], packed[4 * m + 1], packed[4 * m + 2], packed[4 * m + 3]};
+        } else *reinterpret_cast<UInt2*>(out) = UInt2{packed[0], packed[1]};
+    } else if (row < q.rows) {
+        Float4* dst = reinterpret_cast<Float4*>(p.partial + (item * q.all_rows + row) * D + d);
+#pragma unroll
+        for (int m = 0; m < N / 4; ++m) dst[m] = Float4{o[4 * m], o[4 * m + 1], o[4 * m + 2], o[4 * m + 3]};
+    }
+}
+__device__ __forceinline__ void store_stat(const Sequence& q, const AttnMxParams& p, int64_t item, int row, float top, float total) {
+    if (p.splits > 1 && row < q.rows) *reinterpret_cast<float2*>(p.stat + (item * q.all_rows + row) * 2) = float2{top, total};
+}
+
+// A workgroup's place: ids 8 apart are on one XCD, and those that read the same keys for other rows follow each other there.
+struct Place { int item, row_tile, split, g, b; };
+__device__ __forceinline__ Place place_of(const AttnMxParams& p) {
+    const unsigned item = blockIdx.y * 8 + (blockIdx.x & 7), head = item / static_cast<unsigned>(p.splits), b = head / static_cast<unsigned>(p.Hkv);
+    return {static_cast<int>(item), static_cast<int>(blockIdx.x >> 3), static_cast<int>(item - head * p.splits), static_cast<int>(head - b * p.Hkv), static_cast<int>(b)};
+}
+
+// ---- few rows: the wavefronts of a workgroup share the rows and deal the keys out among themselves ----------------------------------
+// Bound by the cache's bytes.  Every wavefront streams pages of its own, 16 bytes a lane and page of keys and of values, the next four pages in
+// flight while four are worked on; no barrier until the end.
 template <int D, int MB, int NP, bool CAP>
 __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
-                                                                     AttnMxParams p) {
-    constexpr int TILES = D / 16, BLOCKS = D / 32;                 // tiles of the output; scale blocks of a row
-    __shared__ float exchange[TM_WAVES * D / 16 * 4 * 64];
+                                                                     const int32_t* __restrict__ block_table, AttnMxParams p) {
+    constexpr int TILES = D / 16;
+    __shared__ float exchange[TM_WAVES * TILES * 4 * 64];
     __shared__ float stats[TM_WAVES][MB][16][2];
-    // Workgroups that read the same keys for other rows run next to each other on the same XCD (ids 8 apart).
-    const int id = blockIdx.x, item = id / (8 * p.row_tiles) * 8 + (id & 7), row_tile = (id >> 3) % p.row_tiles;
-    if (item >= p.items) return;
-    const int split = item % p.splits, g = item / p.splits % p.Hkv, b = item / p.splits / p.Hkv;
+    const Place at = place_of(p);
+    if (at.item >= p.items) return;
+    const int g = at.g, b = at.b, row0 = at.row_tile * 16 * MB;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row16 = lane & 15, quad = lane >> 4;
-    int P = prefix_len[b], n = n_nodes[b];
-    if (P < 0 || n < 0 || n > p.K || static_cast<int64_t>(P) + n > static_cast<int64_t>(p.max_pages) * GRAFT_PAGE_SIZE) n = 0;
-    const int rows = n * p.G, all_rows = p.K * p.G, row0 = row_tile * 16 * MB, L = P + n;
-    const int64_t out_b = static_cast<int64_t>(b) * p.K * p.Hkv * p.G * D;
-    auto out_at = [&](int row) {
-        const int node = row / p.G;
-        return out_b + (static_cast<int64_t>(node) * p.Hkv * p.G + g * p.G + (row - node * p.G)) * D;
-    };
-    if (row0 >= rows) {                                            // uniform: padding nodes only
-        if (p.splits == 1)
-            for (int i = threadIdx.x; i < 16 * MB * (D / 8); i += TM_THREADS) {
-                const int row = row0 + i / (D / 8);
-                if (row < all_rows) *reinterpret_cast<UInt4*>(p.out + out_at(row) + i % (D / 8) * 8) = UInt4{0, 0, 0, 0};
-            }
+    Sequence q = sequence_of(b, prefix_len[b], n_nodes[b], block_table, p, D);
+    if (row0 >= q.rows) {                          // uniform
+        if (p.splits == 1) zero_rows(q, p, g, row0, 16 * MB, D);
         return;
     }
-
-    // queries
     Query query[MB];
     int node[MB];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
         const int row = row0 + mb * 16 + row16;
-        node[mb] = row < rows ? row / p.G : 0;
-        float x[32];
-        const bool there = row < rows && quad < BLOCKS;
-        const UInt4* src = reinterpret_cast<const UInt4*>(p.q + (there ? out_at(row) + quad * 32 : 0));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const UInt4 u = src[i];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[i * 8 + j * 2] = there ? __uint_as_float(u[j] << 16) * p.sign : 0.0f;
-                x[i * 8 + j * 2 + 1] = there ? __uint_as_float(u[j] & 0xFFFF0000u) * p.sign : 0.0f;
-            }
-        }
-        query[mb] = split_query(x);
+        node[mb] = row < q.rows ? node_of(p, row) : 0;
+        query[mb] = load_query<D>(q, p, g, row, quad * 32);
     }
-
-    // the pages that some node sees, and from which token on every node sees all of the prefix
-    const int32_t* pos = p.pos ? p.pos + static_cast<int64_t>(b) * p.K : nullptr;
-    int first_page = 0, all_see = 0;
-    if (p.window > 0) {
-        int low = 0x7FFFFFFF, high = -0x7FFFFFFF;
-        for (int i = lane; i < n; i += 64) {
-            const int at = pos ? pos[i] : P + i;
-            low = at < low ? at : low;
-            high = at > high ? at : high;
-        }
-#pragma unroll
-        for (int s = 32; s > 0; s >>= 1) {
-            const int l2 = __shfl_xor(low, s), h2 = __shfl_xor(high, s);
-            low = l2 < low ? l2 : low;
-            high = h2 > high ? h2 : high;
-        }
-        const int64_t from = static_cast<int64_t>(low) - p.window + 1, all = static_cast<int64_t>(high) - p.window + 1;
-        const int64_t from_in = from < 0 ? 0 : from > P ? P : from;
-        first_page = __builtin_amdgcn_readfirstlane(static_cast<int>(from_in) / GRAFT_PAGE_SIZE);
-        all_see = __builtin_amdgcn_readfirstlane(static_cast<int>(all < 0 ? 0 : all > P ? P : all));
-    }
-    const int end_page = (L + GRAFT_PAGE_SIZE - 1) / GRAFT_PAGE_SIZE;
-    const int tiles = (end_page - first_page + NP - 1) / NP;
-    const int tile_end = static_cast<int>(static_cast<int64_t>(tiles) * (split + 1) / p.splits);
-    int tile = static_cast<int>(static_cast<int64_t>(tiles) * split / p.splits) + wave;
-
-    const int32_t* table = p.block_table + static_cast<int64_t>(b) * p.max_pages;
+    if (p.window > 0) look_back(q, p.window, lane);
+    const Units units(q, NP * GRAFT_PAGE_SIZE, at.split * TM_WAVES + wave, p.splits * TM_WAVES);   // (a piece of the keys for each wavefront)
+    const int page0 = q.first_page + units.first * NP;
     const unsigned char *k_head = p.k_cache + g * p.head_stride, *v_head = p.v_cache + g * p.head_stride;
-    const int k_block = quad & (BLOCKS - 1);                       // (D = 64: lanes past the row's end have zeros of the query)
-    const int k_at = row16 * (D / 2) + k_block * 16, ks_at = mx_scale_at<D>(row16, k_block);
-    const int v_at = lane * (D / 8), vs_at = mx_scale_at<D>(quad * 4, row16 * TILES / 32);
-    using Held = Pages<D, NP>;
-    auto load = [&](int t) {
+    const LaneAt<D> lane_at(lane);
+    struct Held {
+        UInt4 k[NP];
+        unsigned k_scale[NP];
+        ValuePage<D> v[NP];
+    };
+    auto load = [&](PageIds& ids, int i0) {
         Held h;
+        const int page = units.unit(i0) * NP;
+        ids.seek(page);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const int at = first_page + t * NP + i;
-            const int64_t page = static_cast<int64_t>(table[at < end_page ? at : end_page - 1]) * p.page_stride;
-            const unsigned char *k = k_head + page, *v = v_head + page;
-            h.k[i] = *reinterpret_cast<const UInt4*>(k + k_at);
-            h.k_scale[i] = k[ks_at];
-            h.v[i] = *reinterpret_cast<const typename Held::V*>(v + v_at);
-            h.v_scale[i] = *reinterpret_cast<const unsigned*>(v + vs_at);
+            const u64 run = ids.offset(page + i, p.page_stride);
+            const __amdgpu_buffer_rsrc_t k = run_of<D>(k_head + run);
+            h.k[i] = __builtin_bit_cast(UInt4, __builtin_amdgcn_raw_buffer_load_b128(k, lane_at.k, 0, 0));
+            h.k_scale[i] = __builtin_amdgcn_raw_buffer_load_b8(k, lane_at.k_scale, 0, 0);
+            h.v[i].load(run_of<D>(v_head + run), lane_at.v, lane_at.v_scale);
         }
         return h;
     };
 
-    Float4 acc[MB][TILES];
-    float top[MB], sum[MB];
+    Softmax<TILES> soft[MB];
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-        top[mb] = TM_LOW;
-        sum[mb] = 0.0f;
-#pragma unroll
-        for (int m = 0; m < TILES; ++m) acc[mb][m] = Float4{0, 0, 0, 0};
-    }
-
-    auto step = [&](int t, Held& h) {
-        const int first = (first_page + t * NP) * GRAFT_PAGE_SIZE;
-        const bool masked = first + NP * GRAFT_PAGE_SIZE > P || first < all_see;
-        unsigned no_number = 0;                                    // bit 4 i + r: a value of token 4 quad + r of page i is none
-        if (masked) {
-            // Values of tokens behind the last one and values that are no numbers become small ones, which a probability of 0
-            // takes out; rows that see one of the latter get NaN as its score.
+    for (int mb = 0; mb < MB; ++mb) soft[mb].clear();
+    Sight sight[MB];
+    auto step = [&](int i0, Held& h, auto masks) {
+        constexpr bool MASKS = decltype(masks)::value;
+        const int first = (page0 + units.unit(i0) * NP) * GRAFT_PAGE_SIZE;
+        unsigned no_number = 0;
+        if constexpr (MASKS) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const int at = first_page + t * NP + i, token = first + i * GRAFT_PAGE_SIZE + quad * 4;
-                const unsigned char* v = v_head + static_cast<int64_t>(table[at < end_page ? at : end_page - 1]) * p.page_stride;
-                unsigned any = 0;
-#pragma unroll
-                for (int c = 0; c < BLOCKS; ++c) {
-                    const unsigned s4 = *reinterpret_cast<const unsigned*>(v + mx_scale_at<D>(quad * 4, c));
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) any |= ((s4 >> (8 * r)) & 255u) == MX_NAN ? 1u << r : 0u;
-                }
-                no_number |= any << (4 * i);
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (token + r >= L || (any >> r & 1)) h.v_scale[i] = (h.v_scale[i] & ~(255u << (8 * r))) | 2u << (8 * r);
+                no_number |= no_numbers(h.v[i].scale, quad) << (4 * i);
+                h.v[i].keep_numbers(first + i * GRAFT_PAGE_SIZE + quad * 4, q.L);
             }
         }
         Bf8 prob[MB][NP / 2];
+        Float4 s[MB][NP];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) scores(h.k, h.k_scale, query[mb], CAP ? 0.0f : soft[mb].start(), s[mb]);
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-            Float4 s[NP];
-#pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                const Int8 key = {static_cast<int>(h.k[i][0]), static_cast<int>(h.k[i][1]), static_cast<int>(h.k[i][2]), static_cast<int>(h.k[i][3]), 0, 0, 0, 0};
-                auto part = [&](int j) {
-                    const UInt6 u = query[mb].part[j];
-                    return Int8{static_cast<int>(u[0]), static_cast<int>(u[1]), static_cast<int>(u[2]), static_cast<int>(u[3]),
-                                static_cast<int>(u[4]), static_cast<int>(u[5]), 0, 0};
-                };
-                s[i] = Float4{0, 0, 0, 0};
-                s[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, part(2), s[i], 4, 2, 0, h.k_scale[i], 2, query[mb].bytes);
-                s[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, part(1), s[i], 4, 2, 0, h.k_scale[i], 1, query[mb].bytes);
-                s[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, part(0), s[i], 4, 2, 0, h.k_scale[i], 0, query[mb].bytes);
-            }
-            if constexpr (CAP) {
-#pragma unroll
-                for (int i = 0; i < NP; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        s[i][r] = __builtin_fmaf(__builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[i][r] * p.cap_in) + 1.0f), -2.0f * p.cap_out, p.cap_out);
-            }
-            if (masked) {
-                u64 word[2] = {~0ull, ~0ull};
-                if (p.mask) {
-                    const u64* w = p.mask + (static_cast<int64_t>(b) * p.K + node[mb]) * GRAFT_MASK_WORDS;
-                    word[0] = w[0];
-                    word[1] = w[1];
-                }
-                const int at = p.window > 0 ? pos ? pos[node[mb]] : P + node[mb] : 0;
-#pragma unroll
-                for (int i = 0; i < NP; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int token = first + i * GRAFT_PAGE_SIZE + quad * 4 + r, j = token - P;
-                        bool sees = token < P;
-                        if (token >= P && j < n) sees = p.mask ? (word[j >> 6] >> (j & 63)) & 1 : j <= node[mb];
-                        if (p.window > 0 && sees) {
-                            const int64_t place = token < P ? token : pos ? pos[j] : token;
-                            sees = at - place < p.window;
-                        }
-                        s[i][r] = !sees ? -__builtin_inff() : (no_number >> (4 * i + r) & 1) ? __builtin_nanf("") : s[i][r];
-                    }
-            }
-            float most = s[0][0];
-#pragma unroll
-            for (int i = 0; i < NP; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) most = __builtin_fmaxf(most, s[i][r]);
-            if constexpr (!CAP) most *= p.factor;
-            most = rows_max_f32(most);
-            if (__builtin_amdgcn_ballot_w64(most > top[mb] + TM_SLACK) != 0) {
-                const float now = __builtin_fmaxf(most, top[mb]), shrink = __builtin_amdgcn_exp2f(top[mb] - now);
-                top[mb] = now;
-                sum[mb] *= shrink;
-#pragma unroll
-                for (int m = 0; m < TILES; ++m) acc[mb][m] *= shrink;
-            }
-            float x[NP][4];
-#pragma unroll
-            for (int i = 0; i < NP; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    x[i][r] = __builtin_amdgcn_exp2f(CAP ? s[i][r] - top[mb] : __builtin_fmaf(s[i][r], p.factor, -top[mb]));
-                    sum[mb] += x[i][r];
-                }
-#pragma unroll
-            for (int i = 0; i < NP; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) prob[mb][i / 2][(i & 1) * 4 + r] = static_cast<__bf16>(x[i][r]);
+            if constexpr (CAP) cap_scores<NP>(s[mb], p.cap, soft[mb].start());
+            if constexpr (MASKS) mask_scores<NP>(s[mb], q, sight[mb], first, quad, no_number);
         }
-        // values: two neighbouring tiles come out of a conversion, four tokens each of two pages make an operand
+        to_probabilities<MB, NP, MASKS, TILES>(s, i0 == units.whole, soft, prob);
 #pragma unroll
-        for (int i2 = 0; i2 < NP / 2; ++i2) {
-            float scale[2][4];
+        for (int i = 0; i < NP / 2; ++i) {
+            UInt2 low[TILES];
+            value_operands<D>(h.v[2 * i], [&](int m, UInt2 v) { low[m] = v; });
+            value_operands<D>(h.v[2 * i + 1], [&](int m, UInt2 v) {
+                const Bf8 both = __builtin_bit_cast(Bf8, UInt4{low[m][0], low[m][1], v[0], v[1]});
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) scale[i][r] = mx_scale((h.v_scale[2 * i2 + i] >> (8 * r)) & 255u);
-            auto tiles_of = [&](auto pair) {
-                constexpr int M = decltype(pair)::value;
-                unsigned lo[4], hi[4];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    unsigned c[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if constexpr (D == 128) c[r] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(h.v[2 * i2 + i][r], scale[i][r], M));
-                        else if (r & 1) c[r] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(h.v[2 * i2 + i][r / 2], scale[i][r], 2 + M));
-                        else c[r] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(h.v[2 * i2 + i][r / 2], scale[i][r], M));
-                    }
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        lo[2 * i + r] = __builtin_amdgcn_perm(c[2 * r + 1], c[2 * r], 0x05040100);
-                        hi[2 * i + r] = __builtin_amdgcn_perm(c[2 * r + 1], c[2 * r], 0x07060302);
-                    }
-                }
-                const Bf8 even = __builtin_bit_cast(Bf8, UInt4{lo[0], lo[1], lo[2], lo[3]}), odd = __builtin_bit_cast(Bf8, UInt4{hi[0], hi[1], hi[2], hi[3]});
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb) {
-                    acc[mb][2 * M] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, prob[mb][i2], acc[mb][2 * M], 0, 0, 0);
-                    acc[mb][2 * M + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, prob[mb][i2], acc[mb][2 * M + 1], 0, 0, 0);
-                }
-            };
-            tiles_of(std::integral_constant<int, 0>{});
-            tiles_of(std::integral_constant<int, 1>{});
-            if constexpr (TILES > 4) {
-                tiles_of(std::integral_constant<int, 2>{});
-                tiles_of(std::integral_constant<int, 3>{});
-            }
+                for (int mb = 0; mb < MB; ++mb) soft[mb].acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both, prob[mb][i], soft[mb].acc[m], 0, 0, 0);
+            });
         }
     };
-
-    if (tile < tile_end) {
-        Held here = load(tile);
-        for (; tile < tile_end; tile += TM_WAVES) {
-            const int next = tile + TM_WAVES;
-            Held ahead = load(next < tile_end ? next : tile);
-            step(tile, here);
-            here = ahead;
+    if (units.count > 0) {
+        PageIds ids(q, page0, lane);
+        int i = units.whole;
+        Held here = load(ids, i);
+        auto loop = [&](int end, auto masks) {
+#pragma nounroll
+            for (; i < end; ++i) {
+                const Held ahead = load(ids, i + 1);
+                step(i, here, masks);
+                here = ahead;
+            }
+        };
+        loop(units.whole_end, std::false_type{});
+        if (i < units.end()) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) sight[mb] = sight_of(q, p.window, node[mb], lane);
+            loop(units.end(), std::true_type{});
         }
     }
 
@@ -356,11 +609,11 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
     // their tile is 4 quad + w, D / 16 neighbours in the row.
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
-        float s = sum[mb];
+        float s = soft[mb].sum;
         s += __shfl_xor(s, 16);
         s += __shfl_xor(s, 32);
         if (quad == 0) {
-            stats[wave][mb][row16][0] = top[mb];
+            stats[wave][mb][row16][0] = soft[mb].top;
             stats[wave][mb][row16][1] = s;
         }
     }
@@ -372,12 +625,12 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
         for (int w = 0; w < TM_WAVES; ++w) most = __builtin_fmaxf(most, stats[w][mb][row16][0]);
 #pragma unroll
         for (int w = 0; w < TM_WAVES; ++w) total += stats[w][mb][row16][1] * __builtin_amdgcn_exp2f(stats[w][mb][row16][0] - most);
-        const float shrink = __builtin_amdgcn_exp2f(top[mb] - most);
+        const float shrink = __builtin_amdgcn_exp2f(soft[mb].top - most);
         if (mb > 0) __syncthreads();
 #pragma unroll
         for (int m = 0; m < TILES; ++m)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) exchange[((wave * TILES + m) * 4 + r) * 64 + lane] = acc[mb][m][r] * shrink;
+            for (int r = 0; r < 4; ++r) exchange[((wave * TILES + m) * 4 + r) * 64 + lane] = soft[mb].acc[m][r] * shrink;
         __syncthreads();
         float o[TILES];
 #pragma unroll
@@ -386,71 +639,223 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
 #pragma unroll
             for (int w = 0; w < TM_WAVES; ++w) o[m] += exchange[((w * TILES + m) * 4 + wave) * 64 + lane];
         }
-        const int row = row0 + mb * 16 + row16, d = (quad * 4 + wave) * TILES;
-        if (row >= all_rows) continue;
-        if (p.splits == 1) {
-            const float inv = total == 0.0f || row >= rows ? 0.0f : 1.0f / total;
-            unsigned packed[TILES / 2];
-#pragma unroll
-            for (int m = 0; m < TILES; m += 2) {
-                const Bf2 two = {static_cast<__bf16>(row < rows ? o[m] * inv : 0.0f), static_cast<__bf16>(row < rows ? o[m + 1] * inv : 0.0f)};
-                packed[m / 2] = __builtin_bit_cast(unsigned, two);
-            }
-            if constexpr (D == 128) *reinterpret_cast<UInt4*>(p.out + out_at(row) + d) = UInt4{packed[0], packed[1], packed[2], packed[3]};
-            else *reinterpret_cast<UInt2*>(p.out + out_at(row) + d) = UInt2{packed[0], packed[1]};
-        } else if (row < rows) {
-            const int64_t at = static_cast<int64_t>(item) * all_rows + row;
-            Float4* dst = reinterpret_cast<Float4*>(p.partial + at * D + d);
-#pragma unroll
-            for (int m = 0; m < TILES / 4; ++m) dst[m] = Float4{o[4 * m], o[4 * m + 1], o[4 * m + 2], o[4 * m + 3]};
-            if (wave == 0 && quad == 0) *reinterpret_cast<float2*>(p.stat + at * 2) = float2{most, total};
-        }
+        const int row = row0 + mb * 16 + row16;
+        store_part<D, TILES>(q, p, row_at(q, p, g, row, D), at.item, row, (quad * 4 + wave) * TILES, o, total);
+        if (wave == 0 && quad == 0) store_stat(q, p, at.item, row, most, total);
     }
 }
 
-// The splits' sums of a row, 8 elements a lane.
-template <int D>
-__global__ __launch_bounds__(TM_THREADS) void tree_attn_mx_merge_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
-                                                                        AttnMxParams p) {
-    constexpr int LANES = D / 8;
-    const int b = blockIdx.z, g = blockIdx.y, row = blockIdx.x * (TM_THREADS / LANES) + threadIdx.x / LANES, d = threadIdx.x % LANES * 8;
-    const int all_rows = p.K * p.G;
-    if (row >= all_rows) return;
-    const int P = prefix_len[b];
-    int n = n_nodes[b];
-    if (P < 0 || n < 0 || n > p.K || static_cast<int64_t>(P) + n > static_cast<int64_t>(p.max_pages) * GRAFT_PAGE_SIZE) n = 0;
-    float o[8] = {0, 0, 0, 0, 0, 0, 0, 0}, total = 0.0f;
-    if (row < n * p.G) {
-        const int64_t base = static_cast<int64_t>(b * p.Hkv + g) * p.splits * all_rows + row;
-        float most = TM_LOW;
-        for (int s = 0; s < p.splits; ++s) most = __builtin_fmaxf(most, p.stat[(base + static_cast<int64_t>(s) * all_rows) * 2]);
-        for (int s = 0; s < p.splits; ++s) {
-            const int64_t at = base + static_cast<int64_t>(s) * all_rows;
-            const float2 st = *reinterpret_cast<const float2*>(p.stat + at * 2);
-            const Float4 *src = reinterpret_cast<const Float4*>(p.partial + at * D + d), x = src[0], y = src[1];
-            const float w = __builtin_amdgcn_exp2f(st.x - most);
-            total += st.y * w;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                o[j] += x[j] * w;
-                o[4 + j] += y[j] * w;
+// ---- more rows: the wavefronts of a workgroup have 16 rows each and share keys and values -----------------------------------------------
+// Bound by the matrix cores and the vector units together: 64 tokens x 16 rows are 28 matrix instructions of 16 cycles and a softmax of about 60
+// vector instructions and 16 exponentials, and a matrix instruction takes 8 cycles (bfloat16) or 12 (4 and 6 bits) of the vector units' issue.
+// One wavefront waits for its own products and exponentials in turn, so others have to have work meanwhile: hence 16 rows and 128 registers a
+// wavefront, four wavefronts a SIMD, and nothing of the hot loop in scratch, whose reloads would wait for the loads from memory in front of them.
+// Converting 64 tokens' values is 144 vector instructions: four of the eight wavefronts convert a page each into LDS, the others bring a page's
+// keys, and all of them take keys and values from there.  Two stages' buffers, one barrier a
+// stage: while one is read the next is written, from registers that were loaded a stage ago.
+// 96 nodes x 32 heads over 8 KV heads, 4 sequences, prefix 65536: 360 us, 1.15 PFLOP/s for both products, where a large bfloat16 matrix product
+// reaches 1.3 to 1.4 on the same card.  Two row blocks a wavefront, or 32 x 32 products with their order laid down by hand, which halve the
+// matrix instructions' share of the issue, take 362 and 372 us, and longer where there are few stages.
+constexpr int TR_WAVES = 8, TR_PAGES = 4;          // wavefronts; pages of a stage
+
+// A barrier that waits for a wavefront's LDS operations alone: loads from memory stay on their way.
+__device__ __forceinline__ void workgroup_lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int D, bool CAP>
+__global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
+                                                                             const int32_t* __restrict__ block_table, AttnMxParams p) {
+    constexpr int TILES = D / 16, NP = TR_PAGES;
+    __shared__ UInt4 values[2][NP / 2][TILES][64];
+    __shared__ UInt4 keys[2][NP][64];
+    __shared__ unsigned key_scales[2][64];                         // a byte for each page
+    __shared__ unsigned short none[2][NP][4];                      // no_numbers of a stage's pages, by quad
+    const Place at = place_of(p);
+    if (at.item >= p.items) return;
+    const int g = at.g, b = at.b;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row16 = lane & 15, quad = lane >> 4;
+    const int tile_row0 = at.row_tile * 16 * p.waves, row0 = tile_row0 + wave * 16, row = row0 + row16;
+    Sequence q = sequence_of(b, prefix_len[b], n_nodes[b], block_table, p, D);
+    if (tile_row0 >= q.rows) {                     // uniform
+        if (p.splits == 1) zero_rows(q, p, g, tile_row0, 16 * p.waves, D);
+        return;
+    }
+    const int node = row < q.rows ? node_of(p, row) : 0;
+    const Query query = load_query<D>(q, p, g, row, quad * 32);
+    if (p.window > 0) look_back(q, p.window, lane);
+    const Units units(q, NP * GRAFT_PAGE_SIZE, at.split, p.splits);
+    const int page0 = q.first_page + units.first * NP;
+
+    const unsigned char *k_head = p.k_cache + g * p.head_stride, *v_head = p.v_cache + g * p.head_stride;
+    const LaneAt<D> lane_at(lane);
+    // What this wavefront brings of a stage: the first four a page's values each, the others a page's keys; a wavefront without rows does no more.
+    const bool has_rows = wave < p.waves && row0 < q.rows, converts = wave < NP;
+    const int page_of = wave % NP;
+    const unsigned char* head = converts ? v_head : k_head;
+    const unsigned lane_run = converts ? lane_at.v : lane_at.k, lane_scale = converts ? lane_at.v_scale : lane_at.k_scale & ~3u;
+    UInt4 raw;                                     // (of values with D = 64 the first half)
+    unsigned raw_scale;
+    auto fetch = [&](PageIds& ids, int i0) {
+        const int page = units.unit(i0) * NP;
+        ids.seek(page);
+        const __amdgpu_buffer_rsrc_t run = run_of<D>(head + ids.offset(page + page_of, p.page_stride));
+        raw = __builtin_bit_cast(UInt4, __builtin_amdgcn_raw_buffer_load_b128(run, lane_run, 0, 0));
+        raw_scale = __builtin_amdgcn_raw_buffer_load_b32(run, lane_scale, 0, 0);
+    };
+    auto bring = [&](int i0) {
+        const int buf = i0 & 1;
+        if (converts) {
+            ValuePage<D> page;
+            if constexpr (D == 128) page.four = raw;
+            else page.four = UInt2{raw[0], raw[1]};
+            page.scale = raw_scale;
+            if (i0 >= units.whole_end) {
+                const unsigned any = no_numbers(page.scale, quad);
+                if (row16 == 0) none[buf][wave][quad] = static_cast<unsigned short>(any);
+                page.keep_numbers((page0 + units.unit(i0) * NP + wave) * GRAFT_PAGE_SIZE + quad * 4, q.L);
             }
+            value_operands<D>(page, [&](int m, UInt2 v) { reinterpret_cast<UInt2*>(&values[buf][wave >> 1][m][lane])[wave & 1] = v; });
+        } else {
+            keys[buf][page_of][lane] = raw;
+            reinterpret_cast<unsigned char*>(&key_scales[buf][lane])[page_of] = static_cast<unsigned char>(raw_scale >> (8 * (lane_at.k_scale & 3)));
+        }
+    };
+
+    Softmax<TILES> soft[1];
+    soft[0].clear();
+    Sight sight;
+    auto stage = [&](PageIds& ids, int i0, auto masks) {
+        constexpr bool MASKS = decltype(masks)::value;
+        const int buf = i0 & 1;
+        Float4 s[1][NP];
+        if (has_rows) {
+            UInt4 key[NP];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) key[i] = keys[buf][i][lane];
+            scores(key, key_scales[buf][lane], query, CAP ? 0.0f : soft[0].start(), s[0]);
+        }
+        // (while the matrix cores have these: the next stage's buffer, whose readers have passed the last barrier; behind the last stage nobody
+        // reads what comes there)
+        bring(i0 + 1);
+        fetch(ids, i0 + 2);
+        if (has_rows) {
+            if constexpr (CAP) cap_scores<NP>(s[0], p.cap, soft[0].start());
+            if constexpr (MASKS) {
+                unsigned no_number = 0;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) no_number |= static_cast<unsigned>(none[buf][i][quad]) << (4 * i);
+                mask_scores<NP>(s[0], q, sight, (page0 + units.unit(i0) * NP) * GRAFT_PAGE_SIZE, quad, no_number);
+            }
+            Bf8 prob[1][NP / 2];
+            to_probabilities<1, NP, MASKS, TILES>(s, i0 == units.whole, soft, prob);
+#pragma unroll
+            for (int i = 0; i < NP / 2; ++i)
+#pragma unroll
+                for (int m = 0; m < TILES; ++m)
+                    soft[0].acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf8, values[buf][i][m][lane]), prob[0][i], soft[0].acc[m], 0, 0, 0);
+        }
+        workgroup_lds_barrier();
+    };
+    if (units.count > 0) {                         // uniform over the workgroup
+        PageIds ids(q, page0, lane);
+        int i = units.whole;
+        fetch(ids, i);
+        bring(i);
+        fetch(ids, i + 1);
+        workgroup_lds_barrier();
+#pragma nounroll
+        for (; i < units.whole_end; ++i) stage(ids, i, std::false_type{});
+        if (i < units.end()) {
+            sight = sight_of(q, p.window, node, lane);
+#pragma nounroll
+            for (; i < units.end(); ++i) stage(ids, i, std::true_type{});
         }
     }
+    if (wave >= p.waves) return;                   // (its rows are the next tile's)
+    float total = soft[0].sum;
+    total += __shfl_xor(total, 16);
+    total += __shfl_xor(total, 32);
+    const int64_t out_at = row_at(q, p, g, row, D);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        float o[TILES];
+#pragma unroll
+        for (int m = 0; m < TILES; ++m) o[m] = soft[0].acc[m][r];
+        store_part<D, TILES>(q, p, out_at, at.item, row, (quad * 4 + r) * TILES, o, total);
+    }
+    if (quad == 0) store_stat(q, p, at.item, row, soft[0].top, total);
+}
+
+// The splits' sums of a row, 8 elements a lane: each lane has the weights of every LANES-th split, and eight splits' sums are on their way at a time.
+template <int D>
+__global__ __launch_bounds__(TM_THREADS) void tree_attn_mx_merge_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
+                                                                        const float* __restrict__ partial, const float* __restrict__ stat,
+                                                                        AttnMxParams p) {
+    constexpr int LANES = D / 8, HELD = TM_MAX_SPLITS / LANES, BATCH = 8;
+    const int b = blockIdx.z, g = blockIdx.y, row = blockIdx.x * (TM_THREADS / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES, d = lane * 8;
+    const Sequence q = sequence_of(b, prefix_len[b], n_nodes[b], nullptr, p, D);
+    const bool there = row < q.rows;
+    const int64_t base = static_cast<int64_t>(b * p.Hkv + g) * p.splits * q.all_rows + (there ? row : 0), next = q.all_rows;
+    float weight[HELD], total = 0.0f, most = TM_LOW;
+    float2 st[HELD];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) {
+        const int s = lane + h * LANES;
+        st[h] = s < p.splits && there ? *reinterpret_cast<const float2*>(stat + (base + s * next) * 2) : float2{TM_LOW, 0.0f};
+        most = __builtin_fmaxf(most, st[h].x);
+    }
+#pragma unroll
+    for (int s = LANES / 2; s > 0; s >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, s));
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) {
+        weight[h] = __builtin_amdgcn_exp2f(st[h].x - most);
+        total += st[h].y * weight[h];
+    }
+#pragma unroll
+    for (int s = LANES / 2; s > 0; s >>= 1) total += __shfl_xor(total, s);
+    float o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (there) {                                   // (uniform over a row's lanes)
+#pragma unroll
+        for (int h = 0; h < HELD; ++h)
+            for (int s0 = h * LANES; s0 < min(p.splits, (h + 1) * LANES); s0 += BATCH) {
+                Float4 x[BATCH], y[BATCH];
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j) {
+                    const Float4* src = reinterpret_cast<const Float4*>(partial + (base + min(s0 + j, p.splits - 1) * next) * D + d);
+                    x[j] = src[0];
+                    y[j] = src[1];
+                }
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j) {
+                    const float w = __shfl(weight[h], s0 - h * LANES + j, LANES);
+                    if (s0 + j >= p.splits) continue;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        o[k] += x[j][k] * w;
+                        o[4 + k] += y[j][k] * w;
+                    }
+                }
+            }
+    }
+    if (row >= q.all_rows) return;
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    const int node = row / p.G;
     unsigned packed[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const Bf2 two = {static_cast<__bf16>(o[2 * j] * inv), static_cast<__bf16>(o[2 * j + 1] * inv)};
         packed[j] = __builtin_bit_cast(unsigned, two);
     }
-    const int64_t at = ((static_cast<int64_t>(b) * p.K + node) * p.Hkv * p.G + g * p.G + (row - node * p.G)) * D + d;
-    *reinterpret_cast<UInt4*>(p.out + at) = UInt4{packed[0], packed[1], packed[2], packed[3]};
+    *reinterpret_cast<UInt4*>(p.out + row_at(q, p, g, row, D) + d) = UInt4{packed[0], packed[1], packed[2], packed[3]};
 }
 
 // ---- plan --------------------------------------------------------------------------------------------------------------------------
-struct AttnMxPlan { int row_blocks, row_tiles, splits; };
+struct AttnMxPlan {
+    int row_blocks;                                // of 16 rows for each wavefront of the kernel for few rows, 0: the kernel for more
+    int waves, row_tiles, splits;                  // of a workgroup, that have rows; tiles of a head's rows; splits of the keys
+};
 
 static int compute_units() {
     int dev = 0, n = 0;
@@ -461,24 +866,32 @@ static int compute_units() {
     return n;
 }
 
+// Up to TM_MANY rows a head the kernel for few, in tiles of 32; more the other, with as few workgroups as it takes and rows dealt out evenly.  Both, us, D = 128, 8 KV
+// heads, at prefix 32768 of one sequence and 8192 of 16: 64 rows 35 / 37 and 59 / 61, 128 rows 41 / 45 and 86 / 91, 192 rows 49 / 50 and
+// 124 / 123, 256 rows 57 / 56 and 160 / 144, 384 rows 77 / 69 and 244 / 218.
+constexpr int TM_MANY = 128;
 static AttnMxPlan plan_attn_mx(int32_t B, int32_t K, int32_t Hq, int32_t Hkv, int32_t max_pages) {
-    const int rows = K * (Hq / Hkv);
-    AttnMxPlan best{1, (rows + 15) / 16, 1};
-    if (rows > 16) best = {2, (rows + 31) / 32, 1};
-    const int64_t groups = static_cast<int64_t>(B) * Hkv * best.row_tiles;
+    const int rows = K * (Hq / Hkv), blocks = (rows + 15) / 16;
+    AttnMxPlan plan{blocks > 1 ? 2 : 1, TM_WAVES, (blocks + 1) / 2, 1};
+    if (rows > TM_MANY) {
+        plan.row_blocks = 0;
+        plan.row_tiles = (blocks + TR_WAVES - 1) / TR_WAVES;
+        plan.waves = (blocks + plan.row_tiles - 1) / plan.row_tiles;
+    }
+    const int64_t groups = static_cast<int64_t>(B) * Hkv * plan.row_tiles;
     // two workgroups a compute unit; a split has at least two tiles of four pages for each wavefront
     const int64_t fill = 2 * compute_units(), most = (max_pages + 31) / 32;
     int64_t s = groups >= fill ? 1 : fill / groups;
     if (s > most) s = most;
-    if (s > 64) s = 64;
+    if (s > TM_MAX_SPLITS) s = TM_MAX_SPLITS;
     if (s < 1) s = 1;
-    best.splits = static_cast<int>(s);
-    return best;
+    plan.splits = static_cast<int>(s);
+    return plan;
 }
 
 static bool bad_attn_mx_shape(int32_t B, int32_t K, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_pages) {
     return B < 1 || B > 65535 || K < 1 || K > GRAFT_MAX_NODES || Hkv < 1 || Hkv > 65535 || Hq < Hkv || Hq % Hkv != 0 || Hq / Hkv > 16 ||
-           (D != 64 && D != 128) || max_pages < 1 || max_pages > 262144 || static_cast<int64_t>(B) * Hkv > (1 << 22);
+           (D != 64 && D != 128) || max_pages < 1 || max_pages > 262144 || static_cast<int64_t>(B) * Hkv > (1 << 18);                      // (items in the grid's second dimension)
 }
 
 static size_t attn_mx_bytes(const AttnMxPlan& plan, int32_t B, int32_t K, int32_t Hq, int32_t D) {
@@ -502,7 +915,7 @@ extern "C" int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const 
     if (!q || !k_cache || !v_cache || !block_table || !prefix_len || !n_nodes || !out) return GRAFT_ERR_NULL;
     if (window > 0 && mask && !pos) return GRAFT_ERR_NULL;
     if (page_size != GRAFT_PAGE_SIZE || bad_attn_mx_shape(B, K_max, Hq, Hkv, D, max_pages) || page_stride < mx_run_bytes(D) ||
-        head_stride < mx_run_bytes(D) || page_stride % 16 != 0 || head_stride % 16 != 0 || window < 0)
+        head_stride < mx_run_bytes(D) || page_stride > 0xFFFFFFFFll || page_stride % 16 != 0 || head_stride % 16 != 0 || window < 0)
         return GRAFT_ERR_SHAPE;
     if (!(scale - scale == 0.0f) || !(softcap - softcap == 0.0f) || softcap < 0.0f) return GRAFT_ERR_SHAPE;
     if ((reinterpret_cast<size_t>(q) | reinterpret_cast<size_t>(k_cache) | reinterpret_cast<size_t>(v_cache) | reinterpret_cast<size_t>(out)) & 15)
@@ -515,33 +928,32 @@ extern "C" int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const 
     p.q = static_cast<const unsigned short*>(q);
     p.k_cache = static_cast<const unsigned char*>(k_cache);
     p.v_cache = static_cast<const unsigned char*>(v_cache);
-    p.block_table = block_table;
     p.pos = pos;
     p.mask = reinterpret_cast<const u64*>(mask);
     p.out = static_cast<unsigned short*>(out);
     p.partial = static_cast<float*>(workspace);
     p.stat = p.partial + static_cast<size_t>(B) * K_max * Hq * plan.splits * D;
-    p.page_stride = page_stride;
+    p.page_stride = static_cast<unsigned>(page_stride);
     p.head_stride = head_stride;
-    const float size = scale < 0.0f ? -scale : scale;
-    p.sign = scale > 0.0f ? 1 : scale < 0.0f ? -1 : 0;             // (the running maximum is one of raw scores: their factor is positive)
-    p.factor = p.sign == 0 ? 1.0f : size * LOG2E;
-    if (softcap > 0.0f) {
-        p.cap_in = 2.0f * LOG2E * size / softcap;
-        p.cap_out = softcap * LOG2E;
-    }
-    p.K = K_max; p.Hkv = Hkv; p.G = Hq / Hkv; p.max_pages = max_pages; p.window = window; p.splits = plan.splits; p.row_tiles = plan.row_tiles;
+    p.factor = softcap > 0.0f ? 2.0f * LOG2E * scale / softcap : scale * LOG2E;
+    p.cap = softcap * LOG2E;
+    p.per_group = (65536 + Hq / Hkv - 1) / (Hq / Hkv);
+    p.K = K_max; p.Hkv = Hkv; p.G = Hq / Hkv; p.max_pages = max_pages; p.window = window; p.splits = plan.splits; p.row_tiles = plan.row_tiles; p.waves = plan.waves;
     p.items = B * Hkv * plan.splits;
-    const int64_t blocks = (static_cast<int64_t>(p.items) + 7) / 8 * 8 * plan.row_tiles;
-    if (blocks > 0x7FFFFFFF) return GRAFT_ERR_SHAPE;
+    const dim3 blocks(8 * plan.row_tiles, (p.items + 7) / 8);
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(TM_THREADS), 0, static_cast<hipStream_t>(stream), prefix_len, n_nodes, p);
+        hipLaunchKernelGGL(kernel, blocks, dim3(plan.row_blocks == 0 ? 64 * TR_WAVES : TM_THREADS), 0, static_cast<hipStream_t>(stream), prefix_len, n_nodes, block_table, p);
     };
     auto sized = [&](auto d) {
         constexpr int DIM = decltype(d)::value;
-        if (softcap > 0.0f) { if (plan.row_blocks == 1) launch(tree_attn_mx_kernel<DIM, 1, 4, true>); else launch(tree_attn_mx_kernel<DIM, 2, 4, true>); }
-        else if (plan.row_blocks == 1) launch(tree_attn_mx_kernel<DIM, 1, 4, false>);
-        else launch(tree_attn_mx_kernel<DIM, 2, 4, false>);
+        auto capped = [&](auto cap) {
+            constexpr bool CAP = decltype(cap)::value;
+            if (plan.row_blocks == 0) launch(tree_attn_mx_rows_kernel<DIM, CAP>);
+            else if (plan.row_blocks == 1) launch(tree_attn_mx_kernel<DIM, 1, 4, CAP>);
+            else launch(tree_attn_mx_kernel<DIM, 2, 4, CAP>);
+        };
+        if (softcap > 0.0f) capped(std::true_type{});
+        else capped(std::false_type{});
     };
     if (D == 128) sized(std::integral_constant<int, 128>{});
     else sized(std::integral_constant<int, 64>{});
@@ -549,7 +961,7 @@ extern "C" int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const 
     if (rc != GRAFT_OK || plan.splits == 1) return rc;
     const int per = TM_THREADS / (D / 8);
     const dim3 grid((K_max * p.G + per - 1) / per, Hkv, B);
-    if (D == 128) hipLaunchKernelGGL(tree_attn_mx_merge_kernel<128>, grid, dim3(TM_THREADS), 0, static_cast<hipStream_t>(stream), prefix_len, n_nodes, p);
-    else hipLaunchKernelGGL(tree_attn_mx_merge_kernel<64>, grid, dim3(TM_THREADS), 0, static_cast<hipStream_t>(stream), prefix_len, n_nodes, p);
+    if (D == 128) hipLaunchKernelGGL(tree_attn_mx_merge_kernel<128>, grid, dim3(TM_THREADS), 0, static_cast<hipStream_t>(stream), prefix_len, n_nodes, p.partial, p.stat, p);
+    else hipLaunchKernelGGL(tree_attn_mx_merge_kernel<64>, grid, dim3(TM_THREADS), 0, static_cast<hipStream_t>(stream), prefix_len, n_nodes, p.partial, p.stat, p);
     return check_launch();
 }

@@ -84,6 +84,14 @@ def test_attention(lib, change, code):
     assert _call(lib.graft_tree_attn_mx, ATTN, **change) == code
 
 
+@pytest.mark.parametrize("change,code", [
+    ({"a3": 1 << 32}, SHAPE), ({"a11": 65536}, SHAPE), ({"a11": 65535, "a13": 8, "a14": 8}, SHAPE), ({"a11": 4, "a13": 65536, "a14": 65536}, SHAPE),
+])
+def test_attention_limits(lib, change, code):
+    """Page strides of 2^32 bytes, and more heads of sequences than workgroups are counted in."""
+    assert _call(lib.graft_tree_attn_mx, ATTN, **change) == code
+
+
 def test_attention_workspace(lib):
     w = graft.graft_tree_attn_mx_workspace_bytes
     assert w(1, 4, 8, 2, 64, 4) == 0                       # one split
