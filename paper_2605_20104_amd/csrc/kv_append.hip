@@ -6,8 +6,11 @@
 //
 // Bound by memory: every element is read once and written once.  A lane has 8 elements of a row, 16 lanes (8 with D = 64) a row, whatever
 // the pairing: where partners are R / 2 apart a lane loads its partner's 16 bytes too, from a line that its own request brings to
-// the cache (four lanes of a block of 32 stay neighbours, so a block's largest magnitude takes two lane exchanges).  A workgroup has one
-// token and up to KA_ROWS rows a step of a wavefront's lanes, with the token's cosines and sines in registers for all of them.
+// the cache (four lanes of a block of 32 stay neighbours, so a block's largest magnitude takes two lane exchanges).  A wavefront has the
+// cosines and sines of one token in registers, and loads up to HELD rows a lane before it waits for any.
+// With few tokens the wavefronts of a workgroup share one token's rows; from two tokens a compute unit on each has a token of its
+// own (32 + 2 x 8 bf16 heads of 128, us: 256 tokens 7.6 shared and 9.0 not, 512 tokens 11.5 and 9.3, 16382 tokens 128 and 94).  Stores do not
+// push what is read out of the caches: 90.  402 MB in 90 us are 4.5 TB/s; a copy of that size runs at 5.3.
 #include "mx.h"
 
 namespace graft {
@@ -22,7 +25,7 @@ struct AppendParams {
     int32_t* status;
     int64_t q_stride, k_stride, v_stride;                     // elements from token to token
     int64_t page_stride, token_stride, head_stride;           // elements; bytes in the 4-bit cache
-    int32_t n_pos, R, max_pages, T, Hq, Hkv, rows_per_group;
+    int32_t n_pos, R, max_pages, T, Hq, Hkv;
 };
 
 typedef unsigned Quad4 __attribute__((ext_vector_type(4)));
@@ -38,7 +41,7 @@ template <bool F32> struct Eight {
     __device__ __forceinline__ void store(void* base, int64_t at) const {
         Quad4* p = reinterpret_cast<Quad4*>(static_cast<char*>(base) + at * (F32 ? 4 : 2));
 #pragma unroll
-        for (int i = 0; i < (F32 ? 2 : 1); ++i) p[i] = raw[i];
+        for (int i = 0; i < (F32 ? 2 : 1); ++i) __builtin_nontemporal_store(raw[i], p + i);
     }
     __device__ __forceinline__ float get(int j) const {
         if constexpr (F32) return __uint_as_float(raw[j / 4][j % 4]);
@@ -95,35 +98,40 @@ template <int D> __device__ __forceinline__ void store_mx(unsigned char* run, bo
 // (the arguments of the first trip to memory stand first: they arrive in registers)
 template <int D, bool F32, bool MX, bool INTERLEAVED>
 __global__ __launch_bounds__(KA_THREADS) void kv_append_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
-                                                               const int32_t* __restrict__ pos, int32_t T, AppendParams p) {
-    constexpr int LANES = D / 8, ROWS = KA_THREADS / LANES;
-    const int b = blockIdx.z, i = blockIdx.x;
-    const int32_t P = prefix_len[b], n = n_nodes[b];
-    const int64_t token = static_cast<int64_t>(b) * T + i;
+                                                               const int32_t* __restrict__ pos, int32_t T, bool share, AppendParams p) {
+    constexpr int LANES = D / 8, ROWS = 64 / LANES, HELD = F32 ? 2 : 4, WAVES = KA_THREADS / 64;
+    const int b = blockIdx.y, lane64 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = share ? blockIdx.x : blockIdx.x * WAVES;
+    const int64_t token0 = static_cast<int64_t>(b) * T;
+    // This lane's token's position (of a padding token too: one trip to memory for all three) and page.
+    const int mine = min(first + lane64, T - 1);
+    const int32_t P = prefix_len[b], n = n_nodes[b], pos_mine = pos ? pos[token0 + mine] : 0;
     const bool bad = P < 0 || n < 0 || n > T || static_cast<int64_t>(P) + n > static_cast<int64_t>(p.max_pages) * GRAFT_PAGE_SIZE;
     auto turned = [&](int32_t at) { return p.R == 0 || (at >= 0 && at < p.n_pos); };
-    if (i == 0 && blockIdx.y == 0) {               // a sequence's first workgroup looks at all of its positions
-        __shared__ int32_t wrong[KA_THREADS / 64];
+    if (blockIdx.x == 0) {                         // a sequence's first workgroup looks at all of its positions
+        __shared__ int32_t wrong[WAVES];
         bool off = false;
-        if (!bad) for (int32_t j = threadIdx.x; j < n; j += KA_THREADS) off = off || !turned(pos ? pos[token + j] : P + j);
+        if (!bad) for (int32_t j = threadIdx.x; j < n; j += KA_THREADS) off = off || !turned(pos ? pos[token0 + j] : P + j);
         const bool any = __builtin_amdgcn_ballot_w64(off) != 0;
-        if ((threadIdx.x & 63) == 0) wrong[threadIdx.x >> 6] = any;
+        if (lane64 == 0) wrong[wave] = any;
         __syncthreads();
         if (threadIdx.x == 0) {
             int32_t st = bad;
-            for (int w = 0; w < KA_THREADS / 64; ++w) st |= wrong[w];
+            for (int w = 0; w < WAVES; ++w) st |= wrong[w];
             p.status[b] = st ? GRAFT_STATUS_BAD_LENGTH : 0;
         }
     }
-    if (bad || i >= n) return;
-    const int32_t at = pos ? pos[token] : P + i;
-    if (!turned(at)) return;
-    const int32_t slot = P + i;
-    const int64_t page = p.block_table[static_cast<int64_t>(b) * p.max_pages + slot / GRAFT_PAGE_SIZE];
-    const int in_page = slot & (GRAFT_PAGE_SIZE - 1);
+    if (bad || first >= n) return;
+    const int page_mine = p.block_table[static_cast<int64_t>(b) * p.max_pages + (P + min(mine, n - 1)) / GRAFT_PAGE_SIZE];
 
-    const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES, d = lane * 8, half = p.R / 2;
+    const int lane = threadIdx.x % LANES, row = lane64 / LANES + (share ? wave * ROWS : 0), step = share ? WAVES * ROWS : ROWS, d = lane * 8, half = p.R / 2;
     const bool rotates = d < p.R, second = !INTERLEAVED && d >= half;
+    const int partner = second ? -half : half;     // (elements to the pair's other one)
+    const int rows = p.Hq + 2 * p.Hkv;
+    const int t = share ? 0 : wave, i = first + t, in_page = (P + i) & (GRAFT_PAGE_SIZE - 1);
+    const int32_t at = pos ? __builtin_amdgcn_readlane(pos_mine, t) : P + i;
+    const int64_t page = __builtin_amdgcn_readlane(page_mine, t), token = token0 + i;
+    if (i >= n || !turned(at)) return;
     constexpr int ANGLES = INTERLEAVED ? 4 : 8;
     float c[ANGLES], s[ANGLES];
     if (rotates) {
@@ -134,42 +142,52 @@ __global__ __launch_bounds__(KA_THREADS) void kv_append_kernel(const int32_t* __
             s[j] = second || INTERLEAVED ? angle[half + j] : -angle[half + j];
         }
     }
-    const int partner = second ? -half : half;     // (elements to the pair's other one)
-    const int rows = p.Hq + 2 * p.Hkv, last = min(rows, static_cast<int>(blockIdx.y + 1) * p.rows_per_group);
-    for (int r = blockIdx.y * p.rows_per_group + row; r < last; r += ROWS) {
-        const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.Hkv;
-        const int h = is_q ? r : is_v ? r - p.Hq - p.Hkv : r - p.Hq;
-        const void* src = is_q ? p.q : is_v ? p.v : p.k;
-        const int64_t from = token * (is_q ? p.q_stride : is_v ? p.v_stride : p.k_stride) + static_cast<int64_t>(h) * D + d;
-        Eight<F32> own, other;
-        own.load(src, from);
-        float x[8];
+    for (int r0 = row; r0 < rows; r0 += HELD * step) {
+        Eight<F32> held[HELD], others[HELD];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = own.get(j);
-        if (!is_v && rotates) {
-            if constexpr (INTERLEAVED) {
+        for (int u = 0; u < HELD; ++u) {           // all that is read, before any of it is waited for
+            const int r = r0 + u * step;
+            if (r >= rows) break;
+            const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.Hkv;
+            const void* src = is_q ? p.q : is_v ? p.v : p.k;
+            const int64_t from = token * (is_q ? p.q_stride : is_v ? p.v_stride : p.k_stride) + static_cast<int64_t>(is_q ? r : is_v ? r - p.Hq - p.Hkv : r - p.Hq) * D + d;
+            held[u].load(src, from);
+            if (!INTERLEAVED && !is_v && rotates) others[u].load(src, from + partner);
+        }
 #pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const float a = x[j], o = x[j + 1];
-                    x[j] = turn(a, c[j / 2], o, -s[j / 2]);
-                    x[j + 1] = turn(o, c[j / 2], a, s[j / 2]);
+        for (int u = 0; u < HELD; ++u) {
+            const int r = r0 + u * step;
+            if (r >= rows) break;
+            const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.Hkv;
+            const int h = is_q ? r : is_v ? r - p.Hq - p.Hkv : r - p.Hq;
+            Eight<F32>& own = held[u];
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = own.get(j);
+            if (!is_v && rotates) {
+                if constexpr (INTERLEAVED) {
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        const float a = x[j], o = x[j + 1];
+                        x[j] = turn(a, c[j / 2], o, -s[j / 2]);
+                        x[j + 1] = turn(o, c[j / 2], a, s[j / 2]);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = turn(x[j], c[j], others[u].get(j), s[j]);
                 }
-            } else {
-                other.load(src, from + partner);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = turn(x[j], c[j], other.get(j), s[j]);
+                own.set(x);
             }
-            own.set(x);
-        }
-        if constexpr (MX) {
-            if (!is_q) {                           // (the lanes of a block are together again: some of them may not have rotated)
-                unsigned char* cache = static_cast<unsigned char*>(is_v ? p.v_cache : p.k_cache);
-                store_mx<D>(cache + page * p.page_stride + h * p.head_stride, is_v, in_page, lane, x);
-                continue;
+            if constexpr (MX) {
+                if (!is_q) {                       // (the lanes of a block are together again: some of them may not have rotated)
+                    unsigned char* cache = static_cast<unsigned char*>(is_v ? p.v_cache : p.k_cache);
+                    store_mx<D>(cache + page * p.page_stride + h * p.head_stride, is_v, in_page, lane, x);
+                    continue;
+                }
             }
+            if (is_q) own.store(p.q_out, (token * p.Hq + h) * D + d);
+            else own.store(is_v ? p.v_cache : p.k_cache, page * p.page_stride + in_page * p.token_stride + h * p.head_stride + d);
         }
-        if (is_q) own.store(p.q_out, (token * p.Hq + h) * D + d);
-        else own.store(is_v ? p.v_cache : p.k_cache, page * p.page_stride + in_page * p.token_stride + h * p.head_stride + d);
     }
 }
 
@@ -205,11 +223,10 @@ static int32_t kv_append(AppendParams& p, int32_t B, int32_t D, int32_t interlea
             overlap(p.q_out, out, p.v, spans(p.v_stride, static_cast<int64_t>(p.Hkv) * D)))
             return GRAFT_ERR_SHAPE;
     }
-    const int per_step = KA_THREADS / (D / 8), rows = p.Hq + 2 * p.Hkv;
-    p.rows_per_group = (rows + per_step - 1) / per_step * per_step;
-    const dim3 grid(p.T, (rows + p.rows_per_group - 1) / p.rows_per_group, B);
+    const bool share = tokens < 2 * compute_units();
+    const dim3 grid(share ? p.T : (p.T + KA_THREADS / 64 - 1) / (KA_THREADS / 64), B);
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(KA_THREADS), 0, static_cast<hipStream_t>(stream), p.prefix_len, p.n_nodes, p.pos, p.T, p);
+        hipLaunchKernelGGL(kernel, grid, dim3(KA_THREADS), 0, static_cast<hipStream_t>(stream), p.prefix_len, p.n_nodes, p.pos, p.T, share, p);
     };
     auto pick = [&](auto d, auto f32, auto m) {
         if (interleaved) launch(kv_append_kernel<d, f32, m, true>);
@@ -237,7 +254,7 @@ extern "C" int32_t graft_kv_append(const void* q, const void* k, const void* v, 
                                    void* q_out, int32_t* status, void* stream) {
     if (page_size != GRAFT_PAGE_SIZE) return GRAFT_ERR_SHAPE;
     graft::AppendParams p{q, k, v, q_out, k_cache, v_cache, cos_sin, block_table, prefix_len, n_nodes, pos, status, q_stride, k_stride, v_stride,
-                          page_stride, token_stride, head_stride, n_pos, rot_dim, max_pages, T, Hq, Hkv, 0};
+                          page_stride, token_stride, head_stride, n_pos, rot_dim, max_pages, T, Hq, Hkv};
     return graft::kv_append(p, B, D, interleaved, dtype, false, stream);
 }
 
@@ -249,6 +266,6 @@ extern "C" int32_t graft_kv_append_mx(const void* q, const void* k, const void* 
                                       void* q_out, int32_t* status, void* stream) {
     if (page_size != GRAFT_PAGE_SIZE) return GRAFT_ERR_SHAPE;
     graft::AppendParams p{q, k, v, q_out, k_cache, v_cache, cos_sin, block_table, prefix_len, n_nodes, pos, status, q_stride, k_stride, v_stride,
-                          page_stride, 0, head_stride, n_pos, rot_dim, max_pages, T, Hq, Hkv, 0};
+                          page_stride, 0, head_stride, n_pos, rot_dim, max_pages, T, Hq, Hkv};
     return graft::kv_append(p, B, D, interleaved, dtype, true, stream);
 }

@@ -857,15 +857,6 @@ struct AttnMxPlan {
     int waves, row_tiles, splits;                  // of a workgroup, that have rows; tiles of a head's rows; splits of the keys
 };
 
-static int compute_units() {
-    int dev = 0, n = 0;
-    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) {
-        (void)hipGetLastError();                   // (no device: sizes are asked for all the same)
-        return 256;
-    }
-    return n;
-}
-
 // Up to TM_MANY rows a head the kernel for few, in tiles of 32; more the other, with as few workgroups as it takes and rows dealt out evenly.  Both, us, D = 128, 8 KV
 // heads, at prefix 32768 of one sequence and 8192 of 16: 64 rows 35 / 37 and 59 / 61, 128 rows 41 / 45 and 86 / 91, 192 rows 49 / 50 and
 // 124 / 123, 256 rows 57 / 56 and 160 / 144, 384 rows 77 / 69 and 244 / 218.
