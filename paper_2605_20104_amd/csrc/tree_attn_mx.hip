@@ -197,11 +197,11 @@ __device__ __forceinline__ void zero_rows(const Sequence& q, const AttnMxParams&
     }
 }
 
-// 32 elements of a row's query from `from` on; zeros past the row's end.  Rows that are not there get some row's: what comes of it stays
-// in their column of the products.
+// 32 elements of a row's query from `from` on; zeros past the row's end.  Rows that are not there get padding's or some row's: what comes of
+// it stays in their column of the products, and the load need not wait for the sequence's length.
 template <int D> __device__ __forceinline__ Query load_query(const Sequence& q, const AttnMxParams& p, int g, int row, int from) {
     const bool there = from < D;
-    const UInt4* src = reinterpret_cast<const UInt4*>(p.q + row_at(q, p, g, row < q.rows ? row : 0, D) + (there ? from : 0));
+    const UInt4* src = reinterpret_cast<const UInt4*>(p.q + row_at(q, p, g, row < q.all_rows ? row : 0, D) + (there ? from : 0));
     UInt4 raw[4];
     const unsigned keep = there ? ~0u : 0u;
 #pragma unroll
@@ -288,18 +288,20 @@ __device__ __forceinline__ void scores(const UInt4 (&key)[4], unsigned scales, c
 
 // What a row sees: tree slots (those past the last node taken out), and prefix tokens behind `last`.
 struct Sight {
-    u64 word[2];
+    unsigned word[2 * GRAFT_MASK_WORDS];
     int last;
 };
+__device__ __forceinline__ u64 low_bits(int count) { return count >= 64 ? ~0ull : count <= 0 ? 0ull : (1ull << count) - 1; }
 __device__ __forceinline__ Sight sight_of(const Sequence& q, int window, int node, int lane) {
-    auto low = [](int count) { return count >= 64 ? ~0ull : count <= 0 ? 0ull : (1ull << count) - 1; };
-    Sight x{{low(node + 1), low(node + 1 - 64)}, -1};              // (a chain)
+    u64 word[GRAFT_MASK_WORDS] = {low_bits(node + 1), low_bits(node + 1 - 64)};            // (a chain)
     if (q.mask) {
-        x.word[0] = q.mask[node * GRAFT_MASK_WORDS];
-        x.word[1] = q.mask[node * GRAFT_MASK_WORDS + 1];
+        word[0] = q.mask[node * GRAFT_MASK_WORDS];
+        word[1] = q.mask[node * GRAFT_MASK_WORDS + 1];
     }
-    x.word[0] &= low(q.n);
-    x.word[1] &= low(q.n - 64);
+    word[0] &= low_bits(q.n);
+    word[1] &= low_bits(q.n - 64);
+    Sight x;
+    x.last = -1;
     if (window > 0) {                              // uniform
         const int64_t last = (q.pos ? q.pos[node] : q.P + node) - static_cast<int64_t>(window);
         x.last = static_cast<int>(last < -1 ? -1 : last > q.P ? q.P : last);
@@ -308,31 +310,44 @@ __device__ __forceinline__ Sight sight_of(const Sequence& q, int window, int nod
             for (int j = 0; j < q.n; ++j) {
                 const int place = __builtin_amdgcn_readlane(j < 64 ? at[0] : at[1], j & 63);
                 const u64 bit = place > last ? 0ull : 1ull << (j & 63);
-                if (j < 64) x.word[0] &= ~bit;
-                else x.word[1] &= ~bit;
+                if (j < 64) word[0] &= ~bit;
+                else word[1] &= ~bit;
             }
         }
     }
+    x.word[0] = static_cast<unsigned>(word[0]);
+    x.word[1] = static_cast<unsigned>(word[0] >> 32);
+    x.word[2] = static_cast<unsigned>(word[1]);
+    x.word[3] = static_cast<unsigned>(word[1] >> 32);
     return x;
 }
 
-__device__ __forceinline__ bool sees(const Sequence& q, const Sight& sight, int token) {
-    const int j = token - q.P;
-    const unsigned slot = static_cast<unsigned>((j & 64 ? sight.word[1] : sight.word[0]) >> (j & 63)) & 1u;
-    return j < 0 ? token > sight.last : j < GRAFT_MAX_NODES && slot != 0;
+// Which of 64 tokens from `token` on a row sees, the first in bit 0.
+__device__ __forceinline__ u64 seen(const Sequence& q, const Sight& sight, int token) {
+    const int j = token - q.P, k = j >> 5;         // (the slot of the first token, and its word: negative in the prefix)
+    unsigned w[3] = {0, 0, 0};                     // words k, k + 1, k + 2; none outside the four
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) w[i] = k + i == m ? sight.word[m] : w[i];
+    const u64 slots = __builtin_amdgcn_alignbit(w[1], w[0], j & 31) | static_cast<u64>(__builtin_amdgcn_alignbit(w[2], w[1], j & 31)) << 32;
+    return slots | (low_bits(-j) & ~low_bits(sight.last + 1 - token));
 }
 
-// Where a tile of NP pages from token `first` on is not seen whole by every node: what this lane's row does not see becomes -inf, what it sees and
+// Where a tile of four pages from token `first` on is not seen whole by every node: what this lane's row does not see becomes -inf, what it sees and
 // has a value that is no number becomes NaN (no_number: bit 4 i + r).
-template <int NP>
-__device__ __forceinline__ void mask_scores(Float4 (&s)[NP], const Sequence& q, const Sight& sight, int first, int quad, unsigned no_number) {
+__device__ __forceinline__ void mask_scores(Float4 (&s)[4], const Sequence& q, const Sight& sight, int first, int quad, unsigned no_number) {
+    const u64 see = seen(q, sight, first + quad * 4);
+    if (__builtin_amdgcn_ballot_w64(no_number != 0) != 0) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float x = (no_number >> (4 * i + r) & 1) ? __builtin_nanf("") : s[i][r];
-            s[i][r] = sees(q, sight, first + i * GRAFT_PAGE_SIZE + quad * 4 + r) ? x : -__builtin_inff();
-        }
+            for (int r = 0; r < 4; ++r) s[i][r] = (no_number >> (4 * i + r) & 1) ? __builtin_nanf("") : s[i][r];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[i][r] = (static_cast<unsigned>(see >> (32 * (i / 2))) >> (16 * (i & 1) + r) & 1) ? s[i][r] : -__builtin_inff();
 }
 
 // With a cap c the products are y = 2 log2(e) x / c: c tanh(x / c) = c - 2 c / (2^y + 1), in powers of two, less the row's maximum so far.
@@ -396,32 +411,24 @@ template <int NP> __device__ __forceinline__ void to_operand(const Float4 (&x)[N
 #pragma unroll
         for (int r = 0; r < 4; ++r) prob[i / 2][(i & 1) * 4 + r] = static_cast<__bf16>(x[i][r]);
 }
-// Scores to probabilities.  With ALWAYS, or `first`, the maxima are brought up to date first.  Else they are left as they are as long as the
-// probabilities add up to less than TM_MOST in every lane: they and their sums are floating-point numbers, the same up to a power of
-// two.  (So the common case takes no maximum: an exponential, half a conversion and an addition a score.)
-template <int MB, int NP, bool ALWAYS, int TILES>
-__device__ __forceinline__ void to_probabilities(Float4 (&s)[MB][NP], bool first, Softmax<TILES> (&soft)[MB], Bf8 (&prob)[MB][NP / 2]) {
+// Scores to probabilities.  Maxima are left as they are as long as the row has one and the probabilities add up to less than TM_MOST in every
+// lane: they and their sums are floating-point numbers, the same up to a power of two.  (So the common case takes no
+// maximum: an exponential, half a conversion and an addition a score.)
+template <int MB, int NP, int TILES>
+__device__ __forceinline__ void to_probabilities(Float4 (&s)[MB][NP], Softmax<TILES> (&soft)[MB], Bf8 (&prob)[MB][NP / 2]) {
     Float4 x[MB][NP];
     float sum[MB];
-    if constexpr (ALWAYS) {
+    bool over = false;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        sum[mb] = powers<NP>(s[mb], x[mb]);
+        over = over || soft[mb].top == TM_LOW || sum[mb] > TM_MOST;
+    }
+    if (__builtin_amdgcn_ballot_w64(over) != 0) {
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
             soft[mb].raise(s[mb]);
             sum[mb] = powers<NP>(s[mb], x[mb]);
-        }
-    } else {
-        bool over = first;
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) {
-            sum[mb] = powers<NP>(s[mb], x[mb]);
-            over = over || sum[mb] > TM_MOST;
-        }
-        if (__builtin_amdgcn_ballot_w64(over) != 0) {
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-                soft[mb].raise(s[mb]);
-                sum[mb] = powers<NP>(s[mb], x[mb]);
-            }
         }
     }
 #pragma unroll
@@ -507,6 +514,7 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
     constexpr int TILES = D / 16;
     __shared__ float exchange[TM_WAVES * TILES * 4 * 64];
     __shared__ float stats[TM_WAVES][MB][16][2];
+    __shared__ Sight sights[TM_WAVES][MB][16];
     const Place at = place_of(p);
     if (at.item >= p.items) return;
     const int g = at.g, b = at.b, row0 = at.row_tile * 16 * MB;
@@ -552,7 +560,6 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
     Softmax<TILES> soft[MB];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) soft[mb].clear();
-    Sight sight[MB];
     auto step = [&](int i0, Held& h, auto masks) {
         constexpr bool MASKS = decltype(masks)::value;
         const int first = (page0 + units.unit(i0) * NP) * GRAFT_PAGE_SIZE;
@@ -571,9 +578,9 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
             if constexpr (CAP) cap_scores<NP>(s[mb], p.cap, soft[mb].start());
-            if constexpr (MASKS) mask_scores<NP>(s[mb], q, sight[mb], first, quad, no_number);
+            if constexpr (MASKS) mask_scores(s[mb], q, sights[wave][mb][row16], first, quad, no_number);
         }
-        to_probabilities<MB, NP, MASKS, TILES>(s, i0 == units.whole, soft, prob);
+        to_probabilities<MB, NP, TILES>(s, soft, prob);
 #pragma unroll
         for (int i = 0; i < NP / 2; ++i) {
             UInt2 low[TILES];
@@ -589,6 +596,13 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
         PageIds ids(q, page0, lane);
         int i = units.whole;
         Held here = load(ids, i);
+        if (units.whole_end < units.end()) {       // (now: their trip to memory is that of the first keys)
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                const Sight x = sight_of(q, p.window, node[mb], lane);
+                if (quad == 0) sights[wave][mb][row16] = x;
+            }
+        }
         auto loop = [&](int end, auto masks) {
 #pragma nounroll
             for (; i < end; ++i) {
@@ -598,11 +612,7 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
             }
         };
         loop(units.whole_end, std::false_type{});
-        if (i < units.end()) {
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb) sight[mb] = sight_of(q, p.window, node[mb], lane);
-            loop(units.end(), std::true_type{});
-        }
+        loop(units.end(), std::true_type{});
     }
 
     // The wavefronts' sums are brought to the rows' common maximum and added: wavefront w takes the elements whose place in
@@ -673,6 +683,7 @@ __global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(con
     __shared__ UInt4 keys[2][NP][64];
     __shared__ unsigned key_scales[2][64];                         // a byte for each page
     __shared__ unsigned short none[2][NP][4];                      // no_numbers of a stage's pages, by quad
+    __shared__ Sight sights[TR_WAVES][16];
     const Place at = place_of(p);
     if (at.item >= p.items) return;
     const int g = at.g, b = at.b;
@@ -726,7 +737,6 @@ __global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(con
 
     Softmax<TILES> soft[1];
     soft[0].clear();
-    Sight sight;
     auto stage = [&](PageIds& ids, int i0, auto masks) {
         constexpr bool MASKS = decltype(masks)::value;
         const int buf = i0 & 1;
@@ -742,20 +752,27 @@ __global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(con
         bring(i0 + 1);
         fetch(ids, i0 + 2);
         if (has_rows) {
+            UInt4 four[4];                         // values, on their way from LDS four products ahead
+            auto value = [&](int n) { return values[buf][n / TILES][n % TILES][lane]; };
+#pragma unroll
+            for (int n = 0; n < 4; ++n) four[n] = value(n);
+            __builtin_amdgcn_sched_barrier(0);
             if constexpr (CAP) cap_scores<NP>(s[0], p.cap, soft[0].start());
             if constexpr (MASKS) {
                 unsigned no_number = 0;
 #pragma unroll
                 for (int i = 0; i < NP; ++i) no_number |= static_cast<unsigned>(none[buf][i][quad]) << (4 * i);
-                mask_scores<NP>(s[0], q, sight, (page0 + units.unit(i0) * NP) * GRAFT_PAGE_SIZE, quad, no_number);
+                mask_scores(s[0], q, sights[wave][row16], (page0 + units.unit(i0) * NP) * GRAFT_PAGE_SIZE, quad, no_number);
             }
             Bf8 prob[1][NP / 2];
-            to_probabilities<1, NP, MASKS, TILES>(s, i0 == units.whole, soft, prob);
+            to_probabilities<1, NP, TILES>(s, soft, prob);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < NP / 2; ++i)
-#pragma unroll
-                for (int m = 0; m < TILES; ++m)
-                    soft[0].acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf8, values[buf][i][m][lane]), prob[0][i], soft[0].acc[m], 0, 0, 0);
+            for (int n = 0; n < NP / 2 * TILES; ++n) {
+                soft[0].acc[n % TILES] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf8, four[n & 3]), prob[0][n / TILES], soft[0].acc[n % TILES], 0, 0, 0);
+                if (n + 4 < NP / 2 * TILES) four[n & 3] = value(n + 4);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         workgroup_lds_barrier();
     };
@@ -763,16 +780,17 @@ __global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(con
         PageIds ids(q, page0, lane);
         int i = units.whole;
         fetch(ids, i);
+        if (units.whole_end < units.end()) {       // (now: its trip to memory is that of the first keys)
+            const Sight x = sight_of(q, p.window, node, lane);
+            if (quad == 0) sights[wave][row16] = x;
+        }
         bring(i);
         fetch(ids, i + 1);
         workgroup_lds_barrier();
 #pragma nounroll
         for (; i < units.whole_end; ++i) stage(ids, i, std::false_type{});
-        if (i < units.end()) {
-            sight = sight_of(q, p.window, node, lane);
 #pragma nounroll
-            for (; i < units.end(); ++i) stage(ids, i, std::true_type{});
-        }
+        for (; i < units.end(); ++i) stage(ids, i, std::true_type{});
     }
     if (wave >= p.waves) return;                   // (its rows are the next tile's)
     float total = soft[0].sum;
