@@ -875,14 +875,16 @@ struct AttnMxPlan {
     int waves, row_tiles, splits;                  // of a workgroup, that have rows; tiles of a head's rows; splits of the keys
 };
 
-// Up to TM_MANY rows a head the kernel for few, in tiles of 32; more the other, with as few workgroups as it takes and rows dealt out evenly.  Both, us, D = 128, 8 KV
-// heads, at prefix 32768 of one sequence and 8192 of 16: 64 rows 35 / 37 and 59 / 61, 128 rows 41 / 45 and 86 / 91, 192 rows 49 / 50 and
-// 124 / 123, 256 rows 57 / 56 and 160 / 144, 384 rows 77 / 69 and 244 / 218.
-constexpr int TM_MANY = 128;
+// The kernel for few rows in tiles of 32 rows, unless a head has more than TM_MANY and its tiles alone give every compute unit a workgroup: with work
+// for all, the kernel for more rows converts values for 128 rows at once (with as few workgroups as that takes and rows dealt out
+// evenly); with less, it splits keys further and has more to join.  Few / more, us, D = 128, B x K x Hq over Hkv at a prefix:
+//   4 x 96 x 32/8 at 65536  469 / 360     32 x 64 x 32/8 at 4096  161 / 131    16 x 128 x 32/8 at 8192  278 / 235    4 x 64 x 32/8 at 65536  272 / 253
+//   16 x 48 x 32/8 at 8192  114 / 125     1 x 64 x 40/8 at 32768  58 / 62      1 x 128 x 40/8 at 4096    28 / 35     1 x 40 x 32/8 at 2048   15 / 18
+constexpr int TM_MANY = 192;
 static AttnMxPlan plan_attn_mx(int32_t B, int32_t K, int32_t Hq, int32_t Hkv, int32_t max_pages) {
     const int rows = K * (Hq / Hkv), blocks = (rows + 15) / 16;
     AttnMxPlan plan{blocks > 1 ? 2 : 1, TM_WAVES, (blocks + 1) / 2, 1};
-    if (rows > TM_MANY) {
+    if (rows > TM_MANY && static_cast<int64_t>(B) * Hkv * plan.row_tiles >= compute_units()) {
         plan.row_blocks = 0;
         plan.row_tiles = (blocks + TR_WAVES - 1) / TR_WAVES;
         plan.waves = (blocks + plan.row_tiles - 1) / plan.row_tiles;
