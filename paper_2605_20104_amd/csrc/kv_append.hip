@@ -6,11 +6,12 @@
 //
 // Bound by memory: every element is read once and written once.  A lane has 8 elements of a row, 16 lanes (8 with D = 64) a row, whatever
 // the pairing: where partners are R / 2 apart a lane loads its partner's 16 bytes too, from a line that its own request brings to
-// the cache (four lanes of a block of 32 stay neighbours, so a block's largest magnitude takes two lane exchanges).  A wavefront has the
-// cosines and sines of one token in registers, and loads up to HELD rows a lane before it waits for any.
-// With few tokens the wavefronts of a workgroup share one token's rows; from two tokens a compute unit on each has a token of its
-// own (32 + 2 x 8 bf16 heads of 128, us: 256 tokens 7.6 shared and 9.0 not, 512 tokens 11.5 and 9.3, 16382 tokens 128 and 94).  Stores do not
-// push what is read out of the caches: 90.  402 MB in 90 us are 4.5 TB/s; a copy of that size runs at 5.3.
+// the cache (four lanes of a block of 32 stay neighbours, so a block's largest magnitude takes two lane exchanges).  A lane has the
+// cosines and sines of one token in registers, and loads up to HELD rows before it waits for any.
+// With few tokens the lanes of a workgroup share one token's rows.  From two tokens a compute unit on, a wavefront's groups of lanes have
+// a token each and its steps are the rows: what it writes to the cache is next to each other, also where elements of tokens are interleaved.
+// (32 + 2 x 8 bf16 heads of 128, us: 256 tokens 7.6 shared and 9.0 not, 512 tokens 11.5 and 9.3, 16382 tokens 128 and 90.)  Stores do not push
+// what is read out of the caches: 87.  402 MB in 87 us are 4.6 TB/s; a copy of that size runs at 5.3.
 #include "mx.h"
 
 namespace graft {
@@ -101,11 +102,10 @@ __global__ __launch_bounds__(KA_THREADS) void kv_append_kernel(const int32_t* __
                                                                const int32_t* __restrict__ pos, int32_t T, bool share, AppendParams p) {
     constexpr int LANES = D / 8, ROWS = 64 / LANES, HELD = F32 ? 2 : 4, WAVES = KA_THREADS / 64;
     const int b = blockIdx.y, lane64 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int first = share ? blockIdx.x : blockIdx.x * WAVES;
-    const int64_t token0 = static_cast<int64_t>(b) * T;
-    // This lane's token's position (of a padding token too: one trip to memory for all three) and page.
-    const int mine = min(first + lane64, T - 1);
-    const int32_t P = prefix_len[b], n = n_nodes[b], pos_mine = pos ? pos[token0 + mine] : 0;
+    const int i = share ? blockIdx.x : blockIdx.x * ROWS + lane64 / LANES;     // this lane's token
+    const int64_t token0 = static_cast<int64_t>(b) * T, token = token0 + i;
+    // (the position of a padding token too: one trip to memory for all three)
+    const int32_t P = prefix_len[b], n = n_nodes[b], given = pos ? pos[i < T ? token : token0] : 0;
     const bool bad = P < 0 || n < 0 || n > T || static_cast<int64_t>(P) + n > static_cast<int64_t>(p.max_pages) * GRAFT_PAGE_SIZE;
     auto turned = [&](int32_t at) { return p.R == 0 || (at >= 0 && at < p.n_pos); };
     if (blockIdx.x == 0) {                         // a sequence's first workgroup looks at all of its positions
@@ -121,17 +121,16 @@ __global__ __launch_bounds__(KA_THREADS) void kv_append_kernel(const int32_t* __
             p.status[b] = st ? GRAFT_STATUS_BAD_LENGTH : 0;
         }
     }
-    if (bad || first >= n) return;
-    const int page_mine = p.block_table[static_cast<int64_t>(b) * p.max_pages + (P + min(mine, n - 1)) / GRAFT_PAGE_SIZE];
+    if (bad || i >= n) return;
+    const int32_t at = pos ? given : P + i, slot = P + i;
+    if (!turned(at)) return;
+    const int64_t page = p.block_table[static_cast<int64_t>(b) * p.max_pages + slot / GRAFT_PAGE_SIZE];
+    const int in_page = slot & (GRAFT_PAGE_SIZE - 1);
 
-    const int lane = threadIdx.x % LANES, row = lane64 / LANES + (share ? wave * ROWS : 0), step = share ? WAVES * ROWS : ROWS, d = lane * 8, half = p.R / 2;
+    const int lane = threadIdx.x % LANES, row = share ? wave * ROWS + lane64 / LANES : wave, step = share ? WAVES * ROWS : WAVES, d = lane * 8, half = p.R / 2;
     const bool rotates = d < p.R, second = !INTERLEAVED && d >= half;
     const int partner = second ? -half : half;     // (elements to the pair's other one)
     const int rows = p.Hq + 2 * p.Hkv;
-    const int t = share ? 0 : wave, i = first + t, in_page = (P + i) & (GRAFT_PAGE_SIZE - 1);
-    const int32_t at = pos ? __builtin_amdgcn_readlane(pos_mine, t) : P + i;
-    const int64_t page = __builtin_amdgcn_readlane(page_mine, t), token = token0 + i;
-    if (i >= n || !turned(at)) return;
     constexpr int ANGLES = INTERLEAVED ? 4 : 8;
     float c[ANGLES], s[ANGLES];
     if (rotates) {
@@ -179,7 +178,7 @@ __global__ __launch_bounds__(KA_THREADS) void kv_append_kernel(const int32_t* __
                 own.set(x);
             }
             if constexpr (MX) {
-                if (!is_q) {                       // (the lanes of a block are together again: some of them may not have rotated)
+                if (!is_q) {                       // (the lanes of a block are together: some of them may not have rotated, but none has left)
                     unsigned char* cache = static_cast<unsigned char*>(is_v ? p.v_cache : p.k_cache);
                     store_mx<D>(cache + page * p.page_stride + h * p.head_stride, is_v, in_page, lane, x);
                     continue;
@@ -224,7 +223,8 @@ static int32_t kv_append(AppendParams& p, int32_t B, int32_t D, int32_t interlea
             return GRAFT_ERR_SHAPE;
     }
     const bool share = tokens < 2 * compute_units();
-    const dim3 grid(share ? p.T : (p.T + KA_THREADS / 64 - 1) / (KA_THREADS / 64), B);
+    const int per = share ? 1 : 64 / (D / 8);
+    const dim3 grid((p.T + per - 1) / per, B);
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(KA_THREADS), 0, static_cast<hipStream_t>(stream), p.prefix_len, p.n_nodes, p.pos, p.T, share, p);
     };
