@@ -8,10 +8,11 @@
 // the pairing: where partners are R / 2 apart a lane loads its partner's 16 bytes too, from a line that its own request brings to
 // the cache (four lanes of a block of 32 stay neighbours, so a block's largest magnitude takes two lane exchanges).  A lane has the
 // cosines and sines of one token in registers, and loads up to HELD rows before it waits for any.
-// With few tokens the lanes of a workgroup share one token's rows.  From two tokens a compute unit on, a wavefront's groups of lanes have
+// With few tokens the lanes of a workgroup share one token's rows.  Where that gives three of four compute units a workgroup, a wavefront's groups of lanes have
 // a token each and its steps are the rows: what it writes to the cache is next to each other, also where elements of tokens are interleaved.
-// (32 + 2 x 8 bf16 heads of 128, us: 256 tokens 7.6 shared and 9.0 not, 512 tokens 11.5 and 9.3, 16382 tokens 128 and 90.)  Stores do not push
-// what is read out of the caches: 87.  402 MB in 87 us are 4.6 TB/s; a copy of that size runs at 5.3.
+// (32 + 2 x 8 bf16 heads of 128, us: 512 tokens 6.9 shared and 7.8 not, 1024 tokens 11.5 and 9.0, 16382 tokens 128 and 90.)  Stores do not push
+// what is read out of the caches: 87.  A wait for loads is one for the stores in front of them too, so there 12 rows (8 of float32) are held
+// and not 4: 84.  402 MB in 84 us are 4.8 TB/s.  Fewer rows a workgroup (in more of them) take longer, and so do two batches of rows in turn.
 #include "mx.h"
 
 namespace graft {
@@ -97,12 +98,12 @@ template <int D> __device__ __forceinline__ void store_mx(unsigned char* run, bo
 }
 
 // (the arguments of the first trip to memory stand first: they arrive in registers)
-template <int D, bool F32, bool MX, bool INTERLEAVED>
+template <int D, bool F32, bool MX, bool INTERLEAVED, bool SHARE>
 __global__ __launch_bounds__(KA_THREADS) void kv_append_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
-                                                               const int32_t* __restrict__ pos, int32_t T, bool share, AppendParams p) {
-    constexpr int LANES = D / 8, ROWS = 64 / LANES, HELD = F32 ? 2 : 4, WAVES = KA_THREADS / 64;
+                                                               const int32_t* __restrict__ pos, int32_t T, AppendParams p) {
+    constexpr int LANES = D / 8, ROWS = 64 / LANES, HELD = SHARE ? (F32 ? 2 : 4) : (F32 ? 8 : 12), WAVES = KA_THREADS / 64;
     const int b = blockIdx.y, lane64 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int i = share ? blockIdx.x : blockIdx.x * ROWS + lane64 / LANES;     // this lane's token
+    const int i = SHARE ? blockIdx.x : blockIdx.x * ROWS + lane64 / LANES;     // this lane's token
     const int64_t token0 = static_cast<int64_t>(b) * T, token = token0 + i;
     // (the position of a padding token too: one trip to memory for all three)
     const int32_t P = prefix_len[b], n = n_nodes[b], given = pos ? pos[i < T ? token : token0] : 0;
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(KA_THREADS) void kv_append_kernel(const int32_t* __
     const int64_t page = p.block_table[static_cast<int64_t>(b) * p.max_pages + slot / GRAFT_PAGE_SIZE];
     const int in_page = slot & (GRAFT_PAGE_SIZE - 1);
 
-    const int lane = threadIdx.x % LANES, row = share ? wave * ROWS + lane64 / LANES : wave, step = share ? WAVES * ROWS : WAVES, d = lane * 8, half = p.R / 2;
+    const int lane = threadIdx.x % LANES, row = SHARE ? wave * ROWS + lane64 / LANES : wave, step = SHARE ? WAVES * ROWS : WAVES, d = lane * 8, half = p.R / 2;
     const bool rotates = d < p.R, second = !INTERLEAVED && d >= half;
     const int partner = second ? -half : half;     // (elements to the pair's other one)
     const int rows = p.Hq + 2 * p.Hkv;
@@ -222,15 +223,16 @@ static int32_t kv_append(AppendParams& p, int32_t B, int32_t D, int32_t interlea
             overlap(p.q_out, out, p.v, spans(p.v_stride, static_cast<int64_t>(p.Hkv) * D)))
             return GRAFT_ERR_SHAPE;
     }
-    const bool share = tokens < 2 * compute_units();
-    const int per = share ? 1 : 64 / (D / 8);
+    const int own = 64 / (D / 8), per = tokens < 3 * own * compute_units() / 4 ? 1 : own;      // tokens of a workgroup
+    const bool share = per == 1;
     const dim3 grid((p.T + per - 1) / per, B);
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(KA_THREADS), 0, static_cast<hipStream_t>(stream), p.prefix_len, p.n_nodes, p.pos, p.T, share, p);
+        hipLaunchKernelGGL(kernel, grid, dim3(KA_THREADS), 0, static_cast<hipStream_t>(stream), p.prefix_len, p.n_nodes, p.pos, p.T, p);
     };
     auto pick = [&](auto d, auto f32, auto m) {
-        if (interleaved) launch(kv_append_kernel<d, f32, m, true>);
-        else launch(kv_append_kernel<d, f32, m, false>);
+        if (interleaved) { if (share) launch(kv_append_kernel<d, f32, m, true, true>); else launch(kv_append_kernel<d, f32, m, true, false>); }
+        else if (share) launch(kv_append_kernel<d, f32, m, false, true>);
+        else launch(kv_append_kernel<d, f32, m, false, false>);
     };
     auto typed = [&](auto d) {
         using std::false_type;

@@ -1,4 +1,4 @@
-"""graft_kv_append and graft_kv_append_mx with many tokens (512 and more), which are dealt out another way than few."""
+"""graft_kv_append and graft_kv_append_mx with many tokens (768 and more of D = 128, 1536 of D = 64), which are dealt out another way than few."""
 import numpy as np
 import pytest
 import torch
@@ -11,16 +11,16 @@ from mx_util import read_runs
 pytestmark = pytest.mark.gpu
 
 APPENDS = [  # dtype, B, T, Hq, Hkv, D, R, P, interleaved, layout: odd numbers of tokens and of rows, every rotation, one token of many sequences
-    ("f32", 3, 171, 3, 2, 64, 64, 5, False, "head"), ("bf16", 1, 515, 32, 8, 128, 128, 100, False, "head"), ("bf16", 33, 17, 16, 1, 64, 16, 31, False, "token"),
-    ("f32", 2, 261, 3, 3, 128, 64, 15, True, "gap"), ("bf16", 520, 1, 7, 2, 128, 96, 9, False, "head"), ("bf16", 2, 259, 1, 1, 64, 0, 0, True, "token"),
-    ("bf16", 130, 4, 5, 5, 128, 48, 3, True, "head"),
+    ("f32", 3, 515, 3, 2, 64, 64, 5, False, "head"), ("bf16", 1, 771, 32, 8, 128, 128, 100, False, "head"), ("bf16", 97, 17, 16, 1, 64, 16, 31, False, "token"),
+    ("f32", 2, 389, 3, 3, 128, 64, 15, True, "gap"), ("bf16", 780, 1, 7, 2, 128, 96, 9, False, "head"), ("bf16", 2, 801, 1, 1, 64, 0, 0, True, "token"),
+    ("bf16", 195, 4, 5, 5, 128, 48, 3, True, "head"),
 ]
 
 
 @pytest.mark.parametrize("dtype,B,T,Hq,Hkv,D,R,P,interleaved,layout", APPENDS)
 @pytest.mark.parametrize("fused", [True, False])
 def test_append(dtype, B, T, Hq, Hkv, D, R, P, interleaved, layout, fused):
-    assert B * T >= 512
+    assert B * T * D >= 768 * 128
     few.test_append(dtype, B, T, Hq, Hkv, D, R, P, interleaved, layout, fused)
 
 
@@ -30,7 +30,7 @@ def test_append_mx(dtype, B, T, Hq, Hkv, D, R, P, interleaved):
 
 
 def test_q_in_place():
-    c = few._case(3, "bf16", 2, 301, 20, 2, 128, 128, 9, fused=False, tree=False)
+    c = few._case(3, "bf16", 2, 401, 20, 2, 128, 128, 9, fused=False, tree=False)
     strides = {"page": 16 * 2 * 128, "token": 128, "head": 16 * 128}
     q, k, v = (x.contiguous() for x in c["gpu"])
     angles, place = dev(c["cos_sin"], "f32"), (dev(c["table"]), dev(c["P"]), dev(c["n"]))
@@ -48,10 +48,10 @@ def test_q_in_place():
 @pytest.mark.parametrize("mx", [False, True])
 def test_lengths_and_positions_out_of_range(mx):
     """A bad sequence stays as it was; tokens whose positions are not in the table stay out, their neighbours do not."""
-    B, T, D = 4, 150, 128
-    c = few._case(5, "f32", B, T, 2, 2, D, 64, [0, 1, 10, 20], lengths=[150, 4, 150, 0], tree=False)
-    c["P"][1], c["n"][2] = -1, 151
-    wrong = [3, 5, 64, 149]
+    B, T, D = 4, 200, 128
+    c = few._case(5, "f32", B, T, 2, 2, D, 64, [0, 1, 10, 20], lengths=[200, 4, 200, 0], tree=False)
+    c["P"][1], c["n"][2] = -1, 201
+    wrong = [3, 5, 64, 199]
     c["pos"][0, wrong] = [-1, c["cos_sin"].shape[0], 1 << 30, -(1 << 31)]
     if mx:
         strides, caches = {"page": 2176, "head": 1088}, [torch.full((c["total"], 2, 1088), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(2)]
