@@ -12,7 +12,7 @@
 // a token each and its steps are the rows: what it writes to the cache is next to each other, also where elements of tokens are interleaved.
 // (32 + 2 x 8 bf16 heads of 128, us: 512 tokens 6.9 shared and 7.8 not, 1024 tokens 11.5 and 9.0, 16382 tokens 128 and 90.)  Stores do not push
 // what is read out of the caches: 87.  A wait for loads is one for the stores in front of them too, so there 12 rows (8 of float32) are held
-// and not 4: 84.  402 MB in 84 us are 4.8 TB/s.  Fewer rows a workgroup (in more of them) take longer, and so do two batches of rows in turn.
+// and not 4: 84.  411 MB in 84 us are 4.9 TB/s.  Fewer rows a workgroup (in more of them) take longer, and so do two batches of rows in turn.
 #include "mx.h"
 
 namespace graft {

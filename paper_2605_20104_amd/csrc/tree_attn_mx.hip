@@ -506,8 +506,11 @@ __device__ __forceinline__ Place place_of(const AttnMxParams& p) {
 }
 
 // ---- few rows: the wavefronts of a workgroup share the rows and deal the keys out among themselves ----------------------------------
-// Bound by the cache's bytes.  Every wavefront streams pages of its own, 16 bytes a lane and page of keys and of values, the next four pages in
-// flight while four are worked on; no barrier until the end.
+// With one block of rows bound by the cache's bytes: 32 sequences of up to 16384 tokens, 8 heads of 128, 434 MB in 86 us, 5.0 TB/s (all 16384 tokens long:
+// 5.3, and as much with one or two more tiles in flight; a plain read of long pieces reaches 6.3).  With two by the issue of instructions,
+// and where keys are few by the trips to memory in front of the first tile (3 us) and the joining of sums (2 us).  Every wavefront
+// streams pages of its own, 16 bytes a lane and page of keys and of values, the next four pages in flight while four are worked on; no barrier until the
+// end.  The next tile's loads come behind this one's scores, with masks behind its probabilities, when registers are free: no scratch memory.
 template <int D, int MB, int NP, bool CAP>
 __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
                                                                      const int32_t* __restrict__ block_table, AttnMxParams p) {
@@ -560,7 +563,7 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
     Softmax<TILES> soft[MB];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) soft[mb].clear();
-    auto step = [&](int i0, Held& h, auto masks) {
+    auto step = [&](PageIds& ids, int i0, Held& h, auto masks) {   // and h becomes the next tile
         constexpr bool MASKS = decltype(masks)::value;
         const int first = (page0 + units.unit(i0) * NP) * GRAFT_PAGE_SIZE;
         unsigned no_number = 0;
@@ -575,12 +578,15 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
         Float4 s[MB][NP];
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) scores(h.k, h.k_scale, query[mb], CAP ? 0.0f : soft[mb].start(), s[mb]);
+        Held ahead;                                // (from here on: this tile's keys have left their registers, with masks its scores too)
+        if constexpr (!MASKS) ahead = load(ids, i0 + 1);
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
             if constexpr (CAP) cap_scores<NP>(s[mb], p.cap, soft[mb].start());
             if constexpr (MASKS) mask_scores(s[mb], q, sights[wave][mb][row16], first, quad, no_number);
         }
         to_probabilities<MB, NP, TILES>(s, soft, prob);
+        if constexpr (MASKS) ahead = load(ids, i0 + 1);
 #pragma unroll
         for (int i = 0; i < NP / 2; ++i) {
             UInt2 low[TILES];
@@ -591,6 +597,7 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
                 for (int mb = 0; mb < MB; ++mb) soft[mb].acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both, prob[mb][i], soft[mb].acc[m], 0, 0, 0);
             });
         }
+        h = ahead;
     };
     if (units.count > 0) {
         PageIds ids(q, page0, lane);
@@ -606,9 +613,7 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
         auto loop = [&](int end, auto masks) {
 #pragma nounroll
             for (; i < end; ++i) {
-                const Held ahead = load(ids, i + 1);
-                step(i, here, masks);
-                here = ahead;
+                step(ids, i, here, masks);
             }
         };
         loop(units.whole_end, std::false_type{});
@@ -656,14 +661,15 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
 }
 
 // ---- more rows: the wavefronts of a workgroup have 16 rows each and share keys and values -----------------------------------------------
-// Bound by the matrix cores and the vector units together: 64 tokens x 16 rows are 28 matrix instructions of 16 cycles and a softmax of about 60
-// vector instructions and 16 exponentials, and a matrix instruction takes 8 cycles (bfloat16) or 12 (4 and 6 bits) of the vector units' issue.
+// Bound by the matrix cores and the vector units together: 64 tokens x 16 rows are 28 matrix instructions of 16 cycles, and with a wavefront's share of
+// what is done for all 67 vector instructions and 16 exponentials; a matrix instruction takes 8 cycles (bfloat16) or 12 (4 and 6 bits) of the vector
+// units' issue, so four wavefronts need 2800 cycles of it for 1790 of the matrix cores.  A stage takes 3500.
 // One wavefront waits for its own products and exponentials in turn, so others have to have work meanwhile: hence 16 rows and 128 registers a
 // wavefront, four wavefronts a SIMD, and nothing of the hot loop in scratch, whose reloads would wait for the loads from memory in front of them.
-// Converting 64 tokens' values is 144 vector instructions: four of the eight wavefronts convert a page each into LDS, the others bring a page's
+// Converting 64 tokens' values is 164 vector instructions: four of the eight wavefronts convert a page each into LDS, the others bring a page's
 // keys, and all of them take keys and values from there.  Two stages' buffers, one barrier a
 // stage: while one is read the next is written, from registers that were loaded a stage ago.
-// 96 nodes x 32 heads over 8 KV heads, 4 sequences, prefix 65536: 360 us, 1.15 PFLOP/s for both products, where a large bfloat16 matrix product
+// 96 nodes x 32 heads over 8 KV heads, 4 sequences, prefix 65536: 355 us, 1.15 PFLOP/s for both products, where a large bfloat16 matrix product
 // reaches 1.3 to 1.4 on the same card.  Two row blocks a wavefront, or 32 x 32 products with their order laid down by hand, which halve the
 // matrix instructions' share of the issue, take 362 and 372 us, and longer where there are few stages.
 constexpr int TR_WAVES = 8, TR_PAGES = 4;          // wavefronts; pages of a stage
@@ -752,11 +758,14 @@ __global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(con
         bring(i0 + 1);
         fetch(ids, i0 + 2);
         if (has_rows) {
-            UInt4 four[4];                         // values, on their way from LDS four products ahead
+            constexpr bool AHEAD = !MASKS && !CAP;  // values on their way from LDS three products ahead (masks and the cap leave no registers for it)
+            UInt4 three[3];
             auto value = [&](int n) { return values[buf][n / TILES][n % TILES][lane]; };
+            if constexpr (AHEAD) {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) four[n] = value(n);
-            __builtin_amdgcn_sched_barrier(0);
+                for (int n = 0; n < 3; ++n) three[n] = value(n);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             if constexpr (CAP) cap_scores<NP>(s[0], p.cap, soft[0].start());
             if constexpr (MASKS) {
                 unsigned no_number = 0;
@@ -766,12 +775,15 @@ __global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(con
             }
             Bf8 prob[1][NP / 2];
             to_probabilities<1, NP, TILES>(s, soft, prob);
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (AHEAD) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int n = 0; n < NP / 2 * TILES; ++n) {
-                soft[0].acc[n % TILES] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf8, four[n & 3]), prob[0][n / TILES], soft[0].acc[n % TILES], 0, 0, 0);
-                if (n + 4 < NP / 2 * TILES) four[n & 3] = value(n + 4);
-                __builtin_amdgcn_sched_barrier(0);
+                const UInt4 v = !AHEAD ? value(n) : three[n % 3];
+                soft[0].acc[n % TILES] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf8, v), prob[0][n / TILES], soft[0].acc[n % TILES], 0, 0, 0);
+                if constexpr (AHEAD) {
+                    if (n + 3 < NP / 2 * TILES) three[n % 3] = value(n + 3);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
         }
         workgroup_lds_barrier();
@@ -807,7 +819,8 @@ __global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(con
     if (quad == 0) store_stat(q, p, at.item, row, soft[0].top, total);
 }
 
-// The splits' sums of a row, 8 elements a lane: each lane has the weights of every LANES-th split, and eight splits' sums are on their way at a time.
+// The splits' sums of a row, 8 elements a lane, bound by two trips to memory (4 to 5 us), or with many rows by the 4 D bytes of every row and split
+// (27 MB 5.6 us): each lane has the weights of every LANES-th split, and eight splits' sums are on their way at a time.
 template <int D>
 __global__ __launch_bounds__(TM_THREADS) void tree_attn_mx_merge_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
                                                                         const float* __restrict__ partial, const float* __restrict__ stat,
@@ -878,8 +891,8 @@ struct AttnMxPlan {
 // The kernel for few rows in tiles of 32 rows, unless a head has more than TM_MANY and its tiles alone give every compute unit a workgroup: with work
 // for all, the kernel for more rows converts values for 128 rows at once (with as few workgroups as that takes and rows dealt out
 // evenly); with less, it splits keys further and has more to join.  Few / more, us, D = 128, B x K x Hq over Hkv at a prefix:
-//   4 x 96 x 32/8 at 65536  469 / 360     32 x 64 x 32/8 at 4096  161 / 131    16 x 128 x 32/8 at 8192  278 / 235    4 x 64 x 32/8 at 65536  272 / 253
-//   16 x 48 x 32/8 at 8192  114 / 125     1 x 64 x 40/8 at 32768  58 / 62      1 x 128 x 40/8 at 4096    28 / 35     1 x 40 x 32/8 at 2048   15 / 18
+//   4 x 96 x 32/8 at 65536  461 / 354     32 x 64 x 32/8 at 4096  149 / 129    16 x 128 x 32/8 at 8192  266 / 229    4 x 64 x 32/8 at 65536  266 / 248
+//   16 x 48 x 32/8 at 8192  113 / 124     16 x 64 x 32/8 at 8192  139 / 143    1 x 128 x 40/8 at 4096    27 / 36     1 x 40 x 32/8 at 2048   15 / 18
 constexpr int TM_MANY = 192;
 static AttnMxPlan plan_attn_mx(int32_t B, int32_t K, int32_t Hq, int32_t Hkv, int32_t max_pages) {
     const int rows = K * (Hq / Hkv), blocks = (rows + 15) / 16;
@@ -890,7 +903,9 @@ static AttnMxPlan plan_attn_mx(int32_t B, int32_t K, int32_t Hq, int32_t Hkv, in
         plan.waves = (blocks + plan.row_tiles - 1) / plan.row_tiles;
     }
     const int64_t groups = static_cast<int64_t>(B) * Hkv * plan.row_tiles;
-    // two workgroups a compute unit; a split has at least two tiles of four pages for each wavefront
+    // Two workgroups a compute unit: as many as are at work at a time (with four, us: single tokens of 32 sequences 114 -> 117, of 8 28 -> 35,
+    // 64 x 40 rows at 32768 65 -> 72).  A split has at least two tiles of four pages for each wavefront (with one: 64 rows of 8 heads at 256 tokens 10.2 -> 12.2,
+    // at 2048 14.3 -> 14.6, at 8192 20.7 -> 22.9; with four: at 2048 19.0 -> 19.8).
     const int64_t fill = 2 * compute_units(), most = (max_pages + 31) / 32;
     int64_t s = groups >= fill ? 1 : fill / groups;
     if (s > most) s = most;
