@@ -436,7 +436,7 @@ int32_t graft_prune_select(const int32_t* parent, const int32_t* tokens, const f
  *     k_cache, v_cache, strides, block_table, prefix_len   as in graft_tree_attn, IN/OUT
  *     n_nodes [B]        0 <= n_nodes[b] <= T: lengths of a padded batch
  *     q_out [B,T,Hq,D]   dense; may be q itself where q is dense, and overlaps nothing else
- * T is not bounded by GRAFT_MAX_NODES: prompts are appended by the same call.  Rows of q_out and
+ * T is not bounded by GRAFT_MAX_NODES (it is at most 2^30): prompts are appended by the same call.  Rows of q_out and
  * slots of tokens past n_nodes[b] are left as they were.
  * status [B]: GRAFT_STATUS_BAD_LENGTH if prefix_len or n_nodes is out of range or the tokens
  * exceed the block table (then nothing of the sequence is written), or if a position lies outside
@@ -499,7 +499,8 @@ int32_t graft_kv_gather_mx(const void* k_cache, const void* v_cache, int64_t lay
  *
  * q, out [B,K_max,Hq,D] are bf16.  Queries enter the matrix cores as the sum of three 6-bit numbers: what is
  * left out of an element is up to 2^-14 of the largest of its 32; probabilities are rounded to bf16; sums are
- * fp32.  Rows of padding nodes are zeros, and so are all rows of a sequence whose prefix_len < 0,
+ * fp32.  (Queries times scale, or 2 scale / softcap, in blocks whose largest is below 2^-110 lose more.)  A capped score is off by up to
+ * 2^-20 of the cap.  Rows of padding nodes are zeros, and so are all rows of a sequence whose prefix_len < 0,
  * n_nodes is outside [0,K_max] or tokens exceed the block table.  A key or value block that is NaN makes NaN of
  * elements of the rows that see its token, and of no other row.
  *
@@ -507,8 +508,8 @@ int32_t graft_kv_gather_mx(const void* k_cache, const void* v_cache, int64_t lay
  * run at the same time need one each.  It depends on the current device, as graft_tree_attn_workspace_bytes does.
  *
  * Requires D in {64,128}, Hq % Hkv == 0, Hq/Hkv <= 16, 1 <= K_max <= GRAFT_MAX_NODES, 1 <= max_pages <= 262144,
- * B <= 65535, B * Hkv <= 2^18, page_stride < 2^32 (bytes; the cache itself may be larger), window >= 0, softcap >= 0 and finite, scale
- * finite, q and out 16-byte aligned.
+ * B <= 65535, B * Hkv <= 2^18, page_stride < 2^32 (bytes; the cache itself may be larger), window >= 0, 0 <= softcap <= 1024,
+ * 1.45 scale, with a cap 2.9 scale / softcap, finite in fp32, q and out 16-byte aligned.
  */
 size_t graft_tree_attn_mx_workspace_bytes(int32_t B, int32_t K_max, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_pages);
 

@@ -201,7 +201,7 @@ static int32_t kv_append(AppendParams& p, int32_t B, int32_t D, int32_t interlea
     if ((p.Hq > 0 && (!p.q || !p.q_out)) || (p.R > 0 && !p.cos_sin)) return GRAFT_ERR_NULL;
     if (dtype != GRAFT_F32 && dtype != GRAFT_BF16) return GRAFT_ERR_DTYPE;
     const int64_t align = dtype == GRAFT_F32 ? 4 : 8;          // 16-byte loads
-    if (B < 1 || B > 65535 || p.T < 1 || p.Hq < 0 || p.Hq > 65535 || p.Hkv < 1 || p.Hkv > 65535 || (D != 64 && D != 128) || p.max_pages < 1 ||
+    if (B < 1 || B > 65535 || p.T < 1 || p.T > (1 << 30) || p.Hq < 0 || p.Hq > 65535 || p.Hkv < 1 || p.Hkv > 65535 || (D != 64 && D != 128) || p.max_pages < 1 ||
         p.max_pages > 262144 || p.R < 0 || p.R > D || p.R % 16 != 0 || (p.R > 0 && p.n_pos < 1) || (interleaved != 0 && interleaved != 1) ||
         p.k_stride < static_cast<int64_t>(p.Hkv) * D || p.v_stride < static_cast<int64_t>(p.Hkv) * D || p.k_stride % align != 0 ||
         p.v_stride % align != 0 || (p.Hq > 0 && (p.q_stride < static_cast<int64_t>(p.Hq) * D || p.q_stride % align != 0)))
@@ -215,10 +215,11 @@ static int32_t kv_append(AppendParams& p, int32_t B, int32_t D, int32_t interlea
     if (at & 15) return GRAFT_ERR_SHAPE;
     // A row of q is read and written by one wavefront, so q_out may be q; any other overlap would read what was written.
     const int64_t es = dtype == GRAFT_F32 ? 4 : 2, tokens = static_cast<int64_t>(B) * p.T;
-    if (p.Hq > 0 && !(p.q_out == p.q && p.q_stride == static_cast<int64_t>(p.Hq) * D)) {
+    if (p.Hq > 0) {
+        const bool in_place = p.q_out == p.q && p.q_stride == static_cast<int64_t>(p.Hq) * D;
         const int64_t out = tokens * p.Hq * D * es;
         auto spans = [&](int64_t stride, int64_t row) { return ((tokens - 1) * stride + row) * es; };
-        if (overlap(p.q_out, out, p.q, spans(p.q_stride, static_cast<int64_t>(p.Hq) * D)) ||
+        if ((!in_place && overlap(p.q_out, out, p.q, spans(p.q_stride, static_cast<int64_t>(p.Hq) * D))) ||
             overlap(p.q_out, out, p.k, spans(p.k_stride, static_cast<int64_t>(p.Hkv) * D)) ||
             overlap(p.q_out, out, p.v, spans(p.v_stride, static_cast<int64_t>(p.Hkv) * D)))
             return GRAFT_ERR_SHAPE;

@@ -350,7 +350,8 @@ __device__ __forceinline__ void mask_scores(Float4 (&s)[4], const Sequence& q, c
         for (int r = 0; r < 4; ++r) s[i][r] = (static_cast<unsigned>(see >> (32 * (i / 2))) >> (16 * (i & 1) + r) & 1) ? s[i][r] : -__builtin_inff();
 }
 
-// With a cap c the products are y = 2 log2(e) x / c: c tanh(x / c) = c - 2 c / (2^y + 1), in powers of two, less the row's maximum so far.
+// With a cap c the products are y = 2 log2(e) x / c: c tanh(x / c) = c - 2 c / (2^y + 1), in powers of two, less the row's maximum so far.  The two
+// terms cancel for scores that are small next to the cap: up to 2^-20 c is left as an error, which bounds the cap.
 template <int NP> __device__ __forceinline__ void cap_scores(Float4 (&s)[NP], float cap, float start) {
 #pragma unroll
     for (int i = 0; i < NP; ++i)
@@ -609,6 +610,8 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
                 const Sight x = sight_of(q, p.window, node[mb], lane);
                 if (quad == 0) sights[wave][mb][row16] = x;
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");        // (the other lanes of the wavefront read it)
+            __builtin_amdgcn_wave_barrier();
         }
         auto loop = [&](int end, auto masks) {
 #pragma nounroll
@@ -943,13 +946,14 @@ extern "C" int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const 
     if (page_size != GRAFT_PAGE_SIZE || bad_attn_mx_shape(B, K_max, Hq, Hkv, D, max_pages) || page_stride < mx_run_bytes(D) ||
         head_stride < mx_run_bytes(D) || page_stride > 0xFFFFFFFFll || page_stride % 16 != 0 || head_stride % 16 != 0 || window < 0)
         return GRAFT_ERR_SHAPE;
-    if (!(scale - scale == 0.0f) || !(softcap - softcap == 0.0f) || softcap < 0.0f) return GRAFT_ERR_SHAPE;
+    constexpr float LOG2E = 1.44269504088896340736f;
+    const float factor = softcap > 0.0f ? 2.0f * LOG2E * scale / softcap : scale * LOG2E;
+    if (!(factor - factor == 0.0f) || !(softcap >= 0.0f && softcap <= 1024.0f)) return GRAFT_ERR_SHAPE;
     if ((reinterpret_cast<size_t>(q) | reinterpret_cast<size_t>(k_cache) | reinterpret_cast<size_t>(v_cache) | reinterpret_cast<size_t>(out)) & 15)
         return GRAFT_ERR_SHAPE;
     const AttnMxPlan plan = plan_attn_mx(B, K_max, Hq, Hkv, max_pages);
     const size_t need = attn_mx_bytes(plan, B, K_max, Hq, D);
     if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<size_t>(workspace) & 15))) return GRAFT_ERR_WORKSPACE;
-    constexpr float LOG2E = 1.44269504088896340736f;
     AttnMxParams p{};
     p.q = static_cast<const unsigned short*>(q);
     p.k_cache = static_cast<const unsigned char*>(k_cache);
@@ -961,7 +965,7 @@ extern "C" int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const 
     p.stat = p.partial + static_cast<size_t>(B) * K_max * Hq * plan.splits * D;
     p.page_stride = static_cast<unsigned>(page_stride);
     p.head_stride = head_stride;
-    p.factor = softcap > 0.0f ? 2.0f * LOG2E * scale / softcap : scale * LOG2E;
+    p.factor = factor;
     p.cap = softcap * LOG2E;
     p.per_group = (65536 + Hq / Hkv - 1) / (Hq / Hkv);
     p.K = K_max; p.Hkv = Hkv; p.G = Hq / Hkv; p.max_pages = max_pages; p.window = window; p.splits = plan.splits; p.row_tiles = plan.row_tiles; p.waves = plan.waves;

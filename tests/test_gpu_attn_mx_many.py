@@ -104,6 +104,13 @@ def test_scales(scale):
     _check(c, _run(c))
 
 
+@pytest.mark.parametrize("cap", [1024.0, 0.05])
+@pytest.mark.parametrize("shape", [(8, 100, 12, 4, 128, (200,) * 8), (2, 5, 8, 2, 64, (700, 3))])
+def test_largest_and_small_caps(shape, cap):
+    c = _case(23, *shape, spread=2.0)
+    _check(c, _run(c, cap=cap), cap=cap)
+
+
 def test_error_is_that_of_two_roundings():
     """As with few rows: 2^-8 sqrt(1 / (8 ln 2)) for either of two roundings, 2.35e-3 for both."""
     c = _case(21, 1, 128, 65, 13, 128, (2048,), n=(128,))

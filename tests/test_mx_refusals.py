@@ -92,6 +92,21 @@ def test_attention_limits(lib, change, code):
     assert _call(lib.graft_tree_attn_mx, ATTN, **change) == code
 
 
+@pytest.mark.parametrize("change", [{"a18": 1025.0}, {"a17": 3e38}, {"a18": 1e-39}, {"a17": -3e38, "a18": 0.5}])
+def test_attention_scales(lib, change):
+    """Caps that leave too little of a score, scales whose products with log2(e) do not fit a float."""
+    assert _call(lib.graft_tree_attn_mx, ATTN, **change) == SHAPE
+
+
+@pytest.mark.parametrize("f,args,T,out", [("graft_kv_append", APPEND, "a21", "a27"), ("graft_kv_append_mx", MX, "a20", "a26")])
+def test_append_limits(lib, f, args, T, out):
+    """q in place where keys or values lie in it, and more tokens than are counted in."""
+    f = getattr(lib, f)
+    assert _call(f, args, **{out: P, "a1": P + 1024}) == SHAPE
+    assert _call(f, args, **{out: P, "a2": P + 1024}) == SHAPE
+    assert _call(f, args, **{T: (1 << 30) + 1}) == SHAPE
+
+
 def test_attention_workspace(lib):
     w = graft.graft_tree_attn_mx_workspace_bytes
     assert w(1, 4, 8, 2, 64, 4) == 0                       # one split
