@@ -830,15 +830,26 @@ __global__ __launch_bounds__(TM_THREADS) void tree_attn_mx_merge_kernel(const in
                                                                         AttnMxParams p) {
     constexpr int LANES = D / 8, HELD = TM_MAX_SPLITS / LANES, BATCH = 8;
     const int b = blockIdx.z, g = blockIdx.y, row = blockIdx.x * (TM_THREADS / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES, d = lane * 8;
-    const Sequence q = sequence_of(b, prefix_len[b], n_nodes[b], nullptr, p, D);
-    const bool there = row < q.rows;
-    const int64_t base = static_cast<int64_t>(b * p.Hkv + g) * p.splits * q.all_rows + (there ? row : 0), next = q.all_rows;
-    float weight[HELD], total = 0.0f, most = TM_LOW;
+    const int64_t all_rows = p.K * p.G, base = static_cast<int64_t>(b * p.Hkv + g) * p.splits * all_rows + min(row, static_cast<int>(all_rows) - 1);
+    // What rows that are not there have in the workspace is loaded too, and not used: one trip to memory for lengths, statistics and the first sums.
+    Float4 x[BATCH], y[BATCH];
+    auto load = [&](int s0) {
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+            const Float4* src = reinterpret_cast<const Float4*>(partial + (base + min(s0 + j, p.splits - 1) * all_rows) * D + d);
+            x[j] = src[0];
+            y[j] = src[1];
+        }
+    };
     float2 st[HELD];
 #pragma unroll
+    for (int h = 0; h < HELD; ++h) st[h] = *reinterpret_cast<const float2*>(stat + (base + min(lane + h * LANES, p.splits - 1) * all_rows) * 2);
+    load(0);
+    const Sequence q = sequence_of(b, prefix_len[b], n_nodes[b], nullptr, p, D);
+    float weight[HELD], total = 0.0f, most = TM_LOW;
+#pragma unroll
     for (int h = 0; h < HELD; ++h) {
-        const int s = lane + h * LANES;
-        st[h] = s < p.splits && there ? *reinterpret_cast<const float2*>(stat + (base + s * next) * 2) : float2{TM_LOW, 0.0f};
+        if (lane + h * LANES >= p.splits) st[h] = float2{TM_LOW, 0.0f};
         most = __builtin_fmaxf(most, st[h].x);
     }
 #pragma unroll
@@ -851,35 +862,28 @@ __global__ __launch_bounds__(TM_THREADS) void tree_attn_mx_merge_kernel(const in
 #pragma unroll
     for (int s = LANES / 2; s > 0; s >>= 1) total += __shfl_xor(total, s);
     float o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (there) {                                   // (uniform over a row's lanes)
 #pragma unroll
-        for (int h = 0; h < HELD; ++h)
-            for (int s0 = h * LANES; s0 < min(p.splits, (h + 1) * LANES); s0 += BATCH) {
-                Float4 x[BATCH], y[BATCH];
+    for (int h = 0; h < HELD; ++h)
+        for (int s0 = h * LANES; s0 < min(p.splits, (h + 1) * LANES); s0 += BATCH) {
+            if (s0 > 0) load(s0);
 #pragma unroll
-                for (int j = 0; j < BATCH; ++j) {
-                    const Float4* src = reinterpret_cast<const Float4*>(partial + (base + min(s0 + j, p.splits - 1) * next) * D + d);
-                    x[j] = src[0];
-                    y[j] = src[1];
-                }
+            for (int j = 0; j < BATCH; ++j) {
+                const float w = __shfl(weight[h], s0 - h * LANES + j, LANES);
+                if (s0 + j >= p.splits) continue;
 #pragma unroll
-                for (int j = 0; j < BATCH; ++j) {
-                    const float w = __shfl(weight[h], s0 - h * LANES + j, LANES);
-                    if (s0 + j >= p.splits) continue;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        o[k] += x[j][k] * w;
-                        o[4 + k] += y[j][k] * w;
-                    }
+                for (int k = 0; k < 4; ++k) {
+                    o[k] += x[j][k] * w;
+                    o[4 + k] += y[j][k] * w;
                 }
             }
-    }
+        }
     if (row >= q.all_rows) return;
+    const bool there = row < q.rows;
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     unsigned packed[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const Bf2 two = {static_cast<__bf16>(o[2 * j] * inv), static_cast<__bf16>(o[2 * j + 1] * inv)};
+        const Bf2 two = {static_cast<__bf16>(there ? o[2 * j] * inv : 0.0f), static_cast<__bf16>(there ? o[2 * j + 1] * inv : 0.0f)};
         packed[j] = __builtin_bit_cast(unsigned, two);
     }
     *reinterpret_cast<UInt4*>(p.out + row_at(q, p, g, row, D) + d) = UInt4{packed[0], packed[1], packed[2], packed[3]};
