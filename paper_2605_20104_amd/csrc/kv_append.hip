@@ -8,7 +8,8 @@
 // the pairing: where partners are R / 2 apart a lane loads its partner's 16 bytes too, from a line that its own request brings to
 // the cache (four lanes of a block of 32 stay neighbours, so a block's largest magnitude takes two lane exchanges).  A lane has the
 // cosines and sines of one token in registers, and loads up to HELD rows before it waits for any.
-// With few tokens the lanes of a workgroup share one token's rows.  Where that gives three of four compute units a workgroup, a wavefront's groups of lanes have
+// With few tokens the lanes of a workgroup share one token's rows, and as long as there are compute units to spare several workgroups do (64 + 2 x 4
+// heads, us: 1 or 48 tokens 5.4 -> 4.2; 384 tokens, with two each, 7.1 -> 7.5).  Where that gives three of four compute units a workgroup, a wavefront's groups of lanes have
 // a token each and its steps are the rows: what it writes to the cache is next to each other, also where elements of tokens are interleaved.
 // (32 + 2 x 8 bf16 heads of 128, us: 512 tokens 6.9 shared and 7.8 not, 1024 tokens 11.5 and 9.0, 16382 tokens 128 and 90.)  Stores do not push
 // what is read out of the caches: 87.  A wait for loads is one for the stores in front of them too, so there 12 rows (8 of float32) are held
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(KA_THREADS) void kv_append_kernel(const int32_t* __
     const int32_t P = prefix_len[b], n = n_nodes[b], given = pos ? pos[i < T ? token : token0] : 0;
     const bool bad = P < 0 || n < 0 || n > T || static_cast<int64_t>(P) + n > static_cast<int64_t>(p.max_pages) * GRAFT_PAGE_SIZE;
     auto turned = [&](int32_t at) { return p.R == 0 || (at >= 0 && at < p.n_pos); };
-    if (blockIdx.x == 0) {                         // a sequence's first workgroup looks at all of its positions
+    if (blockIdx.x == 0 && blockIdx.z == 0) {      // a sequence's first workgroup looks at all of its positions
         __shared__ int32_t wrong[WAVES];
         bool off = false;
         if (!bad) for (int32_t j = threadIdx.x; j < n; j += KA_THREADS) off = off || !turned(pos ? pos[token0 + j] : P + j);
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(KA_THREADS) void kv_append_kernel(const int32_t* __
     const int64_t page = p.block_table[static_cast<int64_t>(b) * p.max_pages + slot / GRAFT_PAGE_SIZE];
     const int in_page = slot & (GRAFT_PAGE_SIZE - 1);
 
-    const int lane = threadIdx.x % LANES, row = SHARE ? wave * ROWS + lane64 / LANES : wave, step = SHARE ? WAVES * ROWS : WAVES, d = lane * 8, half = p.R / 2;
+    const int lane = threadIdx.x % LANES, row = SHARE ? (blockIdx.z * WAVES + wave) * ROWS + lane64 / LANES : wave, step = SHARE ? gridDim.z * WAVES * ROWS : WAVES, d = lane * 8, half = p.R / 2;
     const bool rotates = d < p.R, second = !INTERLEAVED && d >= half;
     const int partner = second ? -half : half;     // (elements to the pair's other one)
     const int rows = p.Hq + 2 * p.Hkv;
@@ -226,7 +227,9 @@ static int32_t kv_append(AppendParams& p, int32_t B, int32_t D, int32_t interlea
     }
     const int own = 64 / (D / 8), per = tokens < 3 * own * compute_units() / 4 ? 1 : own;      // tokens of a workgroup
     const bool share = per == 1;
-    const dim3 grid((p.T + per - 1) / per, B);
+    // Few tokens' rows go to several workgroups each, as long as there are compute units without one.
+    const int64_t steps = (p.Hq + 2 * p.Hkv + KA_THREADS / (D / 8) - 1) / (KA_THREADS / (D / 8)), room = compute_units() / tokens;
+    const dim3 grid((p.T + per - 1) / per, B, !share || room < 2 ? 1 : room < steps ? room : steps);
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(KA_THREADS), 0, static_cast<hipStream_t>(stream), p.prefix_len, p.n_nodes, p.pos, p.T, p);
     };
