@@ -9,8 +9,8 @@
 // the cache (four lanes of a block of 32 stay neighbours, so a block's largest magnitude takes two lane exchanges).  A lane has the
 // cosines and sines of one token in registers, and loads up to HELD rows before it waits for any.
 // With few tokens the lanes of a workgroup share one token's rows, and as long as there are compute units to spare several workgroups do (64 + 2 x 4
-// heads, us: 1 or 48 tokens 5.4 -> 4.2; 384 tokens, with two each, 7.1 -> 7.5).  Where that gives three of four compute units a workgroup, a wavefront's groups of lanes have
-// a token each and its steps are the rows: what it writes to the cache is next to each other, also where elements of tokens are interleaved.
+// heads, us: 1 or 48 tokens 5.4 -> 4.2; 384 tokens, with two each, 7.1 -> 7.5).  With so many tokens that three of four compute units get a workgroup all the same, a
+// wavefront's groups of lanes have a token each and its steps are the rows: what it writes to the cache is next to each other, also where elements of tokens are interleaved.
 // (32 + 2 x 8 bf16 heads of 128, us: 512 tokens 6.9 shared and 7.8 not, 1024 tokens 11.5 and 9.0, 16382 tokens 128 and 90.)  Stores do not push
 // what is read out of the caches: 87.  A wait for loads is one for the stores in front of them too, so there 12 rows (8 of float32) are held
 // and not 4: 84.  411 MB in 84 us are 4.9 TB/s.  Fewer rows a workgroup (in more of them) take longer, and so do two batches of rows in turn.

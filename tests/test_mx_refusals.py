@@ -68,6 +68,11 @@ def test_gather(lib, change, code):
     assert _call(lib.graft_kv_gather_mx, GATHER, **change) == code
 
 
+def test_gather_limits(lib):
+    """More rows of a sequence than a launch has lanes for."""
+    assert _call(lib.graft_kv_gather_mx, GATHER, a11=(1 << 31) - 1) == SHAPE
+
+
 # q caches page head table max_pages P n mask pos B K Hq Hkv D page scale cap window out ws bytes stream
 ATTN = [P, P, P, 1088, 544, P, 4, P, P, P, P, 1, 4, 8, 2, 64, 16, 0.125, 0.0, 0, P, None, 0, None]
 
