@@ -5,9 +5,9 @@ namespace graft {
 
 // ---- rows as numbers ---------------------------------------------------------------------------------------------------------------
 // One lane makes 8 numbers of 4 bytes and a scale: bound by what it writes (16388 tokens of 8 heads of 128 to bfloat16, 18 MB in and 67 out:
-// 18.8 us, 4.5 TB/s).  Lanes follow the output, so stores are whole lines; a token's keys of a head are 8 D / 16 bytes in a row, its values pieces of 4 (2 with D = 64) bytes whose
-// neighbours other rows of the launch read.
-// Stores do not push the cache out of the caches (an append of those tokens and this 98.8 -> 93.0 us).
+// 18.8 us, 4.5 TB/s).  Lanes follow the output, so stores are whole lines; a token's keys of a head are 8 D / 16 bytes in a row, its values
+// pieces of 4 (2 with D = 64) bytes whose neighbours other rows of the launch read.  Stores do not push what is read out of the caches (an append
+// of those tokens and this 98.8 -> 93.0 us).
 constexpr int KG_THREADS = 256;
 
 struct GatherParams {

@@ -28,6 +28,7 @@ typedef __bf16 Bf8 __attribute__((ext_vector_type(8)));
 
 constexpr int TM_WAVES = 4, TM_THREADS = 64 * TM_WAVES;
 constexpr int TM_MAX_SPLITS = 64;
+constexpr int64_t TM_CACHED = 208ll << 20;         // bytes that the Infinity Cache keeps between launches
 constexpr float TM_LOW = -3.402823466e38f;         // no score yet: below or equal to every finite score
 constexpr float TM_MOST = 4096.0f;                 // sum of a lane's probabilities of a tile from which on the maximum is raised
 
@@ -231,10 +232,10 @@ template <int D> struct ValuePage {
     using V = std::conditional_t<D == 128, UInt4, UInt2>;
     V four;
     unsigned scale;
-    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t run, unsigned at, unsigned scale_at) {
-        if constexpr (D == 128) four = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(run, at, 0, 0));
-        else four = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(run, at, 0, 0));
-        scale = __builtin_amdgcn_raw_buffer_load_b32(run, scale_at, 0, 0);
+    template <int AUX = 0> __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t run, unsigned at, unsigned scale_at) {
+        if constexpr (D == 128) four = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(run, at, 0, AUX));
+        else four = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(run, at, 0, AUX));
+        scale = __builtin_amdgcn_raw_buffer_load_b32(run, scale_at, 0, AUX);
     }
     // Values of tokens behind the last one and values that are no numbers become small ones, which a probability of 0 takes out.
     __device__ __forceinline__ void keep_numbers(int first_token, int L) {
@@ -507,15 +508,15 @@ __device__ __forceinline__ Place place_of(const AttnMxParams& p) {
 }
 
 // ---- few rows: the wavefronts of a workgroup share the rows and deal the keys out among themselves ----------------------------------
-// With one block of rows bound by the cache's bytes: 32 sequences of up to 16384 tokens, 8 heads of 128, 434 MB in 86 us, 5.0 TB/s (all 16384 tokens long:
-// 5.3, and as much with one or two more tiles in flight; a plain read of long pieces reaches 6.3).  With two by the issue of instructions,
+// With one block of rows bound by the cache's bytes: 32 sequences of up to 16384 tokens, 8 heads of 128, 434 MB in 82 us, 5.3 TB/s (all 16384 tokens long:
+// 5.7, and as much with one or two more tiles in flight; a plain read of long pieces reaches 6.3).  With two by the issue of instructions,
 // and where keys are few by the trips to memory in front of the first tile (3 us) and the joining of sums (2 us).  Every wavefront
 // streams pages of its own, 16 bytes a lane and page of keys and of values, the next four pages in flight while four are worked on; no barrier until the
 // end.  The next tile's loads come behind this one's scores, with masks behind its probabilities, when registers are free: no scratch memory.
-template <int D, int MB, int NP, bool CAP>
+template <int D, int MB, int NP, bool CAP, bool STREAM>
 __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
                                                                      const int32_t* __restrict__ block_table, AttnMxParams p) {
-    constexpr int TILES = D / 16;
+    constexpr int TILES = D / 16, AUX = STREAM ? 2 : 0;            // (2: nontemporal)
     __shared__ float exchange[TM_WAVES * TILES * 4 * 64];
     __shared__ float stats[TM_WAVES][MB][16][2];
     __shared__ Sight sights[TM_WAVES][MB][16];
@@ -554,9 +555,9 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
         for (int i = 0; i < NP; ++i) {
             const u64 run = ids.offset(page + i, p.page_stride);
             const __amdgpu_buffer_rsrc_t k = run_of<D>(k_head + run);
-            h.k[i] = __builtin_bit_cast(UInt4, __builtin_amdgcn_raw_buffer_load_b128(k, lane_at.k, 0, 0));
-            h.k_scale[i] = __builtin_amdgcn_raw_buffer_load_b8(k, lane_at.k_scale, 0, 0);
-            h.v[i].load(run_of<D>(v_head + run), lane_at.v, lane_at.v_scale);
+            h.k[i] = __builtin_bit_cast(UInt4, __builtin_amdgcn_raw_buffer_load_b128(k, lane_at.k, 0, AUX));
+            h.k_scale[i] = __builtin_amdgcn_raw_buffer_load_b8(k, lane_at.k_scale, 0, AUX);
+            h.v[i].template load<AUX>(run_of<D>(v_head + run), lane_at.v, lane_at.v_scale);
         }
         return h;
     };
@@ -974,6 +975,11 @@ extern "C" int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const 
     p.per_group = (65536 + Hq / Hkv - 1) / (Hq / Hkv);
     p.K = K_max; p.Hkv = Hkv; p.G = Hq / Hkv; p.max_pages = max_pages; p.window = window; p.splits = plan.splits; p.row_tiles = plan.row_tiles; p.waves = plan.waves;
     p.items = B * Hkv * plan.splits;
+    // One tile of rows reads every page once: from more than the Infinity Cache holds on, of the pages that there is room for and that windows leave,
+    // loads are nontemporal (us: single tokens of 32 sequences of 16384, 571 MB, 114 -> 106; of 64 of 4096, 286 MB, 47 -> 46; of 8 of 8192,
+    // 71 MB, they would be 19 -> 21).
+    const int64_t pages = window > 0 && window / GRAFT_PAGE_SIZE + K_max / GRAFT_PAGE_SIZE + 3 < max_pages ? window / GRAFT_PAGE_SIZE + K_max / GRAFT_PAGE_SIZE + 3 : max_pages;
+    const bool stream_cache = plan.row_blocks != 0 && plan.row_tiles == 1 && 2 * pages * B * Hkv * mx_run_bytes(D) > TM_CACHED;
     const dim3 blocks(8 * plan.row_tiles, (p.items + 7) / 8);
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, blocks, dim3(plan.row_blocks == 0 ? 64 * TR_WAVES : TM_THREADS), 0, static_cast<hipStream_t>(stream), prefix_len, n_nodes, block_table, p);
@@ -983,8 +989,9 @@ extern "C" int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const 
         auto capped = [&](auto cap) {
             constexpr bool CAP = decltype(cap)::value;
             if (plan.row_blocks == 0) launch(tree_attn_mx_rows_kernel<DIM, CAP>);
-            else if (plan.row_blocks == 1) launch(tree_attn_mx_kernel<DIM, 1, 4, CAP>);
-            else launch(tree_attn_mx_kernel<DIM, 2, 4, CAP>);
+            else if (plan.row_blocks == 1) { if (stream_cache) launch(tree_attn_mx_kernel<DIM, 1, 4, CAP, true>); else launch(tree_attn_mx_kernel<DIM, 1, 4, CAP, false>); }
+            else if (stream_cache) launch(tree_attn_mx_kernel<DIM, 2, 4, CAP, true>);
+            else launch(tree_attn_mx_kernel<DIM, 2, 4, CAP, false>);
         };
         if (softcap > 0.0f) capped(std::true_type{});
         else capped(std::false_type{});

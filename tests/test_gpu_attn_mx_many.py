@@ -111,6 +111,17 @@ def test_largest_and_small_caps(shape, cap):
     _check(c, _run(c, cap=cap), cap=cap)
 
 
+@pytest.mark.parametrize("K,Hq,D", [(1, 8, 128), (1, 32, 64), (8, 8, 128), (7, 6, 64), (2, 2, 128)])
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+def test_tables_with_room_for_more_than_the_caches_hold(K, Hq, D, cap):
+    """Few rows a head over what may be more than 208 MB are read another way."""
+    c = _case(31, 4, K, Hq, 2, D, (700, 3, 64, 1500))
+    c["table"] = np.pad(c["table"], ((0, 0), (0, 26000 - c["table"].shape[1])))
+    assert 2 * 26000 * 4 * 2 * (17 * D // 2) > 208 << 20
+    _check(c, _run(c, cap=cap), cap=cap)
+    _check(c, _run(c, cap=cap, window=50), cap=cap, window=50)
+
+
 def test_error_is_that_of_two_roundings():
     """As with few rows: 2^-8 sqrt(1 / (8 ln 2)) for either of two roundings, 2.35e-3 for both."""
     c = _case(21, 1, 128, 65, 13, 128, (2048,), n=(128,))
