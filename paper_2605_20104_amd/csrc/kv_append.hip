@@ -225,10 +225,11 @@ static int32_t kv_append(AppendParams& p, int32_t B, int32_t D, int32_t interlea
             overlap(p.q_out, out, p.v, spans(p.v_stride, static_cast<int64_t>(p.Hkv) * D)))
             return GRAFT_ERR_SHAPE;
     }
-    const int own = 64 / (D / 8), per = tokens < 3 * own * compute_units() / 4 ? 1 : own;      // tokens of a workgroup
+    const int64_t cus = device_compute_units();
+    const int own = 64 / (D / 8), per = tokens < 3 * own * cus / 4 ? 1 : own;                  // tokens of a workgroup
     const bool share = per == 1;
     // Few tokens' rows go to several workgroups each, as long as there are compute units without one.
-    const int64_t steps = (p.Hq + 2 * p.Hkv + KA_THREADS / (D / 8) - 1) / (KA_THREADS / (D / 8)), room = compute_units() / tokens;
+    const int64_t steps = (p.Hq + 2 * p.Hkv + KA_THREADS / (D / 8) - 1) / (KA_THREADS / (D / 8)), room = cus / tokens;
     const dim3 grid((p.T + per - 1) / per, B, !share || room < 2 ? 1 : room < steps ? room : steps);
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(KA_THREADS), 0, static_cast<hipStream_t>(stream), p.prefix_len, p.n_nodes, p.pos, p.T, p);

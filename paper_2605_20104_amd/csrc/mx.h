@@ -35,14 +35,6 @@ __device__ __forceinline__ unsigned mx_scale_byte(unsigned top) {
 }
 __device__ __forceinline__ float mx_scale(unsigned byte) { return __uint_as_float(byte << 23); }    // (255: the conversions make NaN of it)
 
-// Of the current device.
-inline int compute_units() {
-    int dev = 0, n = 0;
-    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) {
-        (void)hipGetLastError();                   // (no device: sizes are asked for all the same)
-        return 256;
-    }
-    return n;
-}
+int device_compute_units();                       // (tree_attn.hip)
 
 }  // namespace graft

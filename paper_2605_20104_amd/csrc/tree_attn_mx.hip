@@ -513,10 +513,10 @@ __device__ __forceinline__ Place place_of(const AttnMxParams& p) {
 // and where keys are few by the trips to memory in front of the first tile (3 us) and the joining of sums (2 us).  Every wavefront
 // streams pages of its own, 16 bytes a lane and page of keys and of values, the next four pages in flight while four are worked on; no barrier until the
 // end.  The next tile's loads come behind this one's scores, with masks behind its probabilities, when registers are free: no scratch memory.
-template <int D, int MB, int NP, bool CAP, bool STREAM>
+template <int D, int MB, bool CAP, bool STREAM>
 __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
                                                                      const int32_t* __restrict__ block_table, AttnMxParams p) {
-    constexpr int TILES = D / 16, AUX = STREAM ? 2 : 0;            // (2: nontemporal)
+    constexpr int TILES = D / 16, NP = 4, AUX = STREAM ? 2 : 0;    // tiles of the output; pages of a tile of keys; (2: nontemporal)
     __shared__ float exchange[TM_WAVES * TILES * 4 * 64];
     __shared__ float stats[TM_WAVES][MB][16][2];
     __shared__ Sight sights[TM_WAVES][MB][16];
@@ -905,7 +905,7 @@ constexpr int TM_MANY = 192;
 static AttnMxPlan plan_attn_mx(int32_t B, int32_t K, int32_t Hq, int32_t Hkv, int32_t max_pages) {
     const int rows = K * (Hq / Hkv), blocks = (rows + 15) / 16;
     AttnMxPlan plan{blocks > 1 ? 2 : 1, TM_WAVES, (blocks + 1) / 2, 1};
-    if (rows > TM_MANY && static_cast<int64_t>(B) * Hkv * plan.row_tiles >= compute_units()) {
+    if (rows > TM_MANY && static_cast<int64_t>(B) * Hkv * plan.row_tiles >= device_compute_units()) {
         plan.row_blocks = 0;
         plan.row_tiles = (blocks + TR_WAVES - 1) / TR_WAVES;
         plan.waves = (blocks + plan.row_tiles - 1) / plan.row_tiles;
@@ -914,7 +914,7 @@ static AttnMxPlan plan_attn_mx(int32_t B, int32_t K, int32_t Hq, int32_t Hkv, in
     // Two workgroups a compute unit: as many as are at work at a time (with four, us: single tokens of 32 sequences 114 -> 117, of 8 28 -> 35,
     // 64 x 40 rows at 32768 65 -> 72).  A split has at least two tiles of four pages for each wavefront (with one: 64 rows of 8 heads at 256 tokens 10.2 -> 12.2,
     // at 2048 14.3 -> 14.6, at 8192 20.7 -> 22.9; with four: at 2048 19.0 -> 19.8).
-    const int64_t fill = 2 * compute_units(), most = (max_pages + 31) / 32;
+    const int64_t fill = 2 * device_compute_units(), most = (max_pages + 31) / 32;
     int64_t s = groups >= fill ? 1 : fill / groups;
     if (s > most) s = most;
     if (s > TM_MAX_SPLITS) s = TM_MAX_SPLITS;
@@ -978,7 +978,7 @@ extern "C" int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const 
     // One tile of rows reads every page once: from more than the Infinity Cache holds on, of the pages that there is room for and that windows leave,
     // loads are nontemporal (us: single tokens of 32 sequences of 16384, 571 MB, 114 -> 106; of 64 of 4096, 286 MB, 47 -> 46; of 8 of 8192,
     // 71 MB, they would be 19 -> 21).
-    const int64_t pages = window > 0 && window / GRAFT_PAGE_SIZE + K_max / GRAFT_PAGE_SIZE + 3 < max_pages ? window / GRAFT_PAGE_SIZE + K_max / GRAFT_PAGE_SIZE + 3 : max_pages;
+    const int64_t windowed = window / GRAFT_PAGE_SIZE + K_max / GRAFT_PAGE_SIZE + 3, pages = window > 0 && windowed < max_pages ? windowed : max_pages;
     const bool stream_cache = plan.row_blocks != 0 && plan.row_tiles == 1 && 2 * pages * B * Hkv * mx_run_bytes(D) > TM_CACHED;
     const dim3 blocks(8 * plan.row_tiles, (p.items + 7) / 8);
     auto launch = [&](auto kernel) {
@@ -989,9 +989,10 @@ extern "C" int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const 
         auto capped = [&](auto cap) {
             constexpr bool CAP = decltype(cap)::value;
             if (plan.row_blocks == 0) launch(tree_attn_mx_rows_kernel<DIM, CAP>);
-            else if (plan.row_blocks == 1) { if (stream_cache) launch(tree_attn_mx_kernel<DIM, 1, 4, CAP, true>); else launch(tree_attn_mx_kernel<DIM, 1, 4, CAP, false>); }
-            else if (stream_cache) launch(tree_attn_mx_kernel<DIM, 2, 4, CAP, true>);
-            else launch(tree_attn_mx_kernel<DIM, 2, 4, CAP, false>);
+            else if (plan.row_blocks == 1 && stream_cache) launch(tree_attn_mx_kernel<DIM, 1, CAP, true>);
+            else if (plan.row_blocks == 1) launch(tree_attn_mx_kernel<DIM, 1, CAP, false>);
+            else if (stream_cache) launch(tree_attn_mx_kernel<DIM, 2, CAP, true>);
+            else launch(tree_attn_mx_kernel<DIM, 2, CAP, false>);
         };
         if (softcap > 0.0f) capped(std::true_type{});
         else capped(std::false_type{});
