@@ -824,7 +824,7 @@ __global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(con
 }
 
 // The splits' sums of a row, 8 elements a lane, bound by two trips to memory (4 to 5 us), or with many rows by the 4 D bytes of every row and split
-// (27 MB 5.6 us): each lane has the weights of every LANES-th split, and eight splits' sums are on their way at a time.
+// (31 MB 7.5 us): each lane has the weights of every LANES-th split, and eight splits' sums are on their way at a time.
 template <int D>
 __global__ __launch_bounds__(TM_THREADS) void tree_attn_mx_merge_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
                                                                         const float* __restrict__ partial, const float* __restrict__ stat,
