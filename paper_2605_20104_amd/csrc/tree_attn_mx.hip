@@ -823,7 +823,7 @@ __global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(con
     if (quad == 0) store_stat(q, p, at.item, row, soft[0].top, total);
 }
 
-// The splits' sums of a row, 8 elements a lane, bound by two trips to memory (4 to 5 us), or with many rows by the 4 D bytes of every row and split
+// The splits' sums of a row, 8 elements a lane, bound by its launch and a trip to memory (4 to 5 us), or with many rows by the 4 D bytes of every row and split
 // (31 MB 7.5 us): each lane has the weights of every LANES-th split, and eight splits' sums are on their way at a time.
 template <int D>
 __global__ __launch_bounds__(TM_THREADS) void tree_attn_mx_merge_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ n_nodes,
