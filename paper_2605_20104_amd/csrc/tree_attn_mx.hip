@@ -198,8 +198,8 @@ __device__ __forceinline__ void zero_rows(const Sequence& q, const AttnMxParams&
     }
 }
 
-// 32 elements of a row's query from `from` on; zeros past the row's end.  Rows that are not there get padding's or some row's: what comes of
-// it stays in their column of the products, and the load need not wait for the sequence's length.
+// 32 elements of a row's query from `from` on; zeros past the row's end.  Rows that are not there get padding's or some row's, so that the load need
+// not wait for the sequence's length: what comes of it stays in their column of the products, and they have no vote in to_probabilities.
 template <int D> __device__ __forceinline__ Query load_query(const Sequence& q, const AttnMxParams& p, int g, int row, int from) {
     const bool there = from < D;
     const UInt4* src = reinterpret_cast<const UInt4*>(p.q + row_at(q, p, g, row < q.all_rows ? row : 0, D) + (there ? from : 0));
@@ -390,8 +390,8 @@ template <int TILES> struct Softmax {
         for (int m = 0; m < TILES; ++m) acc[m] = Float4{0, 0, 0, 0};
     }
     __device__ __forceinline__ float start() const { return top == TM_LOW ? 0.0f : -top; }
-    // A new maximum, of what the row has seen and these scores.
-    template <int NP> __device__ __forceinline__ void raise(Float4 (&s)[NP]) {
+    // A new maximum, of what the row has seen and these scores, for rows that vote for it; all else stays as it is, to the bit.
+    template <int NP> __device__ __forceinline__ void raise(Float4 (&s)[NP], bool vote) {
         float most = __builtin_fmaxf(s[0][0], s[0][1]);
 #pragma unroll
         for (int i = 0; i < NP; ++i)
@@ -400,7 +400,7 @@ template <int TILES> struct Softmax {
         most = rows_max_f32(most);
         const bool fresh = top == TM_LOW;
         float up = fresh ? most : __builtin_fmaxf(most, 0.0f);
-        if (up == -__builtin_inff()) up = 0.0f;           // (nothing seen yet, and nothing here)
+        if (!vote || up == -__builtin_inff()) up = 0.0f;           // (nothing seen yet, and nothing here)
         else top = (fresh ? 0.0f : top) + up;
         const Shrink shrink(fresh ? 0.0f : -up);
         sum = shrink.of(sum);
@@ -428,23 +428,27 @@ template <int NP> __device__ __forceinline__ void to_operand(const Float4 (&x)[N
 #pragma unroll
         for (int r = 0; r < 4; ++r) prob[i / 2][(i & 1) * 4 + r] = static_cast<__bf16>(x[i][r]);
 }
-// Scores to probabilities.  Maxima are left as they are as long as the row has one and the probabilities add up to less than TM_MOST in every
-// lane: they and their sums are floating-point numbers, the same up to a power of two.  (So the common case takes no
-// maximum: an exponential, half a conversion and an addition a score.)
+// Scores to probabilities.  A row's maximum is left as it is as long as it has one and the probabilities add up to less than TM_MOST in each of its
+// lanes: they and their sums are floating-point numbers, the same up to a power of two.  (So the common case takes no
+// maximum: an exponential, half a conversion and an addition a score.)  A power of two that is no whole one moves where probabilities are
+// rounded, so a row's four lanes decide for that row alone, and rows that are not there (`live`: a bit for each lane whose row is) not at all:
+// a result depends on its row's query and on what the row sees.
 template <int MB, int NP, int TILES>
-__device__ __forceinline__ void to_probabilities(Float4 (&s)[MB][NP], Softmax<TILES> (&soft)[MB], Bf8 (&prob)[MB][NP / 2]) {
+__device__ __forceinline__ void to_probabilities(Float4 (&s)[MB][NP], Softmax<TILES> (&soft)[MB], const u64 (&live)[MB], Bf8 (&prob)[MB][NP / 2]) {
     Float4 x[MB][NP];
     float sum[MB];
-    bool over = false;
+    u64 over[MB], any = 0;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
         sum[mb] = powers<NP>(s[mb], x[mb]);
-        over = over || soft[mb].top == TM_LOW || sum[mb] > TM_MOST;
+        over[mb] = __builtin_amdgcn_ballot_w64(soft[mb].top == TM_LOW || sum[mb] > TM_MOST) & live[mb];
+        any |= over[mb];
     }
-    if (__builtin_amdgcn_ballot_w64(over) != 0) {
+    if (any != 0) {
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-            soft[mb].raise(s[mb]);
+            const u64 half = over[mb] | over[mb] >> 32, votes = (half | half >> 16) & 0xFFFF;
+            soft[mb].raise(s[mb], __builtin_amdgcn_inverse_ballot_w64(votes * 0x0001000100010001ull));     // (the row's, in each of its lanes)
             sum[mb] = powers<NP>(s[mb], x[mb]);
         }
     }
@@ -546,10 +550,12 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
     }
     Query query[MB];
     int node[MB];
+    u64 live[MB];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
         const int row = row0 + mb * 16 + row16;
         node[mb] = row < q.rows ? node_of(p, row) : 0;
+        live[mb] = __builtin_amdgcn_ballot_w64(row < q.rows);
         query[mb] = load_query<D>(q, p, g, row, quad * 32);
     }
     if (p.window > 0) look_back(q, p.window, lane);
@@ -602,7 +608,7 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
             if constexpr (CAP) cap_scores<NP>(s[mb], p.cap, soft[mb].start());
             if constexpr (MASKS) mask_scores(s[mb], q, sights[wave][mb][row16], first, quad, no_number);
         }
-        to_probabilities<MB, NP, TILES>(s, soft, prob);
+        to_probabilities<MB, NP, TILES>(s, soft, live, prob);
         if constexpr (MASKS) ahead = load(ids, i0 + 1);
 #pragma unroll
         for (int i = 0; i < NP / 2; ++i) {
@@ -720,6 +726,7 @@ __global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(con
         return;
     }
     const int node = row < q.rows ? node_of(p, row) : 0;
+    const u64 live[1] = {__builtin_amdgcn_ballot_w64(row < q.rows)};
     const Query query = load_query<D>(q, p, g, row, quad * 32);
     if (p.window > 0) look_back(q, p.window, lane);
     const Units units(q, NP * GRAFT_PAGE_SIZE, at.split, p.splits);
@@ -793,7 +800,7 @@ __global__ __launch_bounds__(64 * TR_WAVES, 4) void tree_attn_mx_rows_kernel(con
                 mask_scores(s[0], q, sights[wave][row16], (page0 + units.unit(i0) * NP) * GRAFT_PAGE_SIZE, quad, no_number);
             }
             Bf8 prob[1][NP / 2];
-            to_probabilities<1, NP, TILES>(s, soft, prob);
+            to_probabilities<1, NP, TILES>(s, soft, live, prob);
             if constexpr (AHEAD) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int n = 0; n < NP / 2 * TILES; ++n) {
