@@ -454,7 +454,8 @@ int32_t graft_kv_append(const void* q, const void* k, const void* v, int64_t q_s
 
 /*
  * The 4-bit cache.  Elements are e2m1 (sign, two bits of exponent, one of mantissa: 0, 0.5, 1, 1.5,
- * 2, 3, 4, 6) in blocks of 32 along D with one scale 2^(byte - 127) each; 255 makes NaN of its block.
+ * 2, 3, 4, 6) in blocks of 32 along D with one scale 2^(byte - 127) each; 255 makes NaN of its block.  (Appends write 2..252 and
+ * 255.  Larger elements of byte 253 or 254 pass what bfloat16 holds: such a block may be taken for infinite.)
  * The 16 tokens that a page holds of one KV head are one run of GRAFT_MX_RUN_BYTES(D) bytes: 8 D
  * bytes of elements, two to a byte, the one of the smaller index in the low half, then D/32 rows of 16 scale bytes, one
  * per token.  Order of a run's elements: keys [token][D]; values [token / 4][part of 16][token % 4]
@@ -478,7 +479,7 @@ int32_t graft_kv_append_mx(const void* q, const void* k, const void* v, int64_t 
 
 /*
  * graft_kv_gather_mx - rows of a 4-bit cache as numbers: k_out, v_out [n_layers,B,T,Hkv,D] of dtype (both
- * types hold every element exactly), row t < count[b] being token start[b] + t (start == NULL: t), rows
+ * types hold every element up to scale byte 252 exactly), row t < count[b] being token start[b] + t (start == NULL: t), rows
  * behind it zeros.  status [B]: GRAFT_STATUS_BAD_LENGTH if start < 0, count outside [0,T] or tokens
  * exceed the block table; then all rows of the sequence are zeros.
  */
@@ -502,7 +503,8 @@ int32_t graft_kv_gather_mx(const void* k_cache, const void* v_cache, int64_t lay
  * fp32.  (Queries times scale, or 2 scale / softcap, in blocks whose largest is below 2^-110 lose more.)  A capped score is off by up to
  * 2^-20 of the cap.  Rows of padding nodes are zeros, and so are all rows of a sequence whose prefix_len < 0,
  * n_nodes is outside [0,K_max] or tokens exceed the block table.  A key or value block that is NaN makes NaN of
- * elements of the rows that see its token, and of no other row.
+ * elements of the rows that see its token, one of scale byte 253 or 254 infinities or NaN, and neither of any other row.
+ * Values past 2^97 may overflow in sums.
  *
  * workspace: at least graft_tree_attn_mx_workspace_bytes(...) bytes (0: NULL will do), 16-byte aligned, scratch; calls that may
  * run at the same time need one each.  It depends on the current device, as graft_tree_attn_workspace_bytes does.

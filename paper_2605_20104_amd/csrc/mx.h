@@ -28,6 +28,7 @@ template <int D> __device__ __forceinline__ int mx_scale_at(int token, int block
 // N(0,1) data: 0.1119 with this border, 0.1155 with the largest kept at 6 or below, 0.1151 with no second case.)  Bytes are held
 // within 2..252: what the elements stand for is finite and normal in float32 and bfloat16.  255, NaN, where an element is no number.
 constexpr unsigned MX_NAN = 255;
+constexpr unsigned MX_TOO_LARGE = 253;             // from here on: elements that bfloat16 does not hold, or NaN
 __device__ __forceinline__ unsigned mx_scale_byte(unsigned top) {
     const int e = static_cast<int>((top + 0x1FFFFFu) >> 23) - 2;
     const unsigned byte = static_cast<unsigned>(e < 2 ? 2 : e > 252 ? 252 : e);

@@ -237,20 +237,20 @@ template <int D> struct ValuePage {
         else four = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(run, at, 0, AUX));
         scale = __builtin_amdgcn_raw_buffer_load_b32(run, scale_at, 0, AUX);
     }
-    // Values of tokens behind the last one and values that are no numbers become small ones, which a probability of 0 takes out.
+    // Values of tokens behind the last one and values that are, or may be, infinite or no numbers become small ones, which a probability of 0 takes out.
     __device__ __forceinline__ void keep_numbers(int first_token, int L) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            if (first_token + r >= L || ((scale >> (8 * r)) & 255u) == MX_NAN) scale = (scale & ~(255u << (8 * r))) | 2u << (8 * r);
+            if (first_token + r >= L || ((scale >> (8 * r)) & 255u) >= MX_TOO_LARGE) scale = (scale & ~(255u << (8 * r))) | 2u << (8 * r);
     }
 };
 
-// Bit r: the value of token 4 quad + r of a page is no number in any of its blocks, which the 16 lanes of a quad hold between them.
+// Bit r: the value of token 4 quad + r of a page is, or may be, infinite or no number in any of its blocks, which the 16 lanes of a quad hold between them.
 __device__ __forceinline__ unsigned no_numbers(unsigned scale, int quad) {
     unsigned any = 0;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const u64 lanes = __builtin_amdgcn_ballot_w64(((scale >> (8 * r)) & 255u) == MX_NAN);
+        const u64 lanes = __builtin_amdgcn_ballot_w64(((scale >> (8 * r)) & 255u) >= MX_TOO_LARGE);
         any |= (lanes >> (16 * quad) & 0xFFFFull) != 0 ? 1u << r : 0u;
     }
     return any;
