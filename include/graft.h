@@ -436,7 +436,8 @@ int32_t graft_prune_select(const int32_t* parent, const int32_t* tokens, const f
  *     k_cache, v_cache, strides, block_table, prefix_len   as in graft_tree_attn, IN/OUT
  *     n_nodes [B]        0 <= n_nodes[b] <= T: lengths of a padded batch
  *     q_out [B,T,Hq,D]   dense; may be q itself where q is dense, and overlaps nothing else
- * T is not bounded by GRAFT_MAX_NODES (it is at most 2^30): prompts are appended by the same call.  Rows of q_out and
+ * T is not bounded by GRAFT_MAX_NODES: prompts are appended by the same call.  (A launch has fewer than 2^32
+ * lanes, D/2 for a token: T is at most 2^26 - 4 with D = 128 and 2^27 - 8 with D = 64.)  Rows of q_out and
  * slots of tokens past n_nodes[b] are left as they were.
  * status [B]: GRAFT_STATUS_BAD_LENGTH if prefix_len or n_nodes is out of range or the tokens
  * exceed the block table (then nothing of the sequence is written), or if a position lies outside

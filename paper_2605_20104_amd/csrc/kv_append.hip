@@ -202,11 +202,13 @@ static int32_t kv_append(AppendParams& p, int32_t B, int32_t D, int32_t interlea
     if ((p.Hq > 0 && (!p.q || !p.q_out)) || (p.R > 0 && !p.cos_sin)) return GRAFT_ERR_NULL;
     if (dtype != GRAFT_F32 && dtype != GRAFT_BF16) return GRAFT_ERR_DTYPE;
     const int64_t align = dtype == GRAFT_F32 ? 4 : 8;          // 16-byte loads
-    if (B < 1 || B > 65535 || p.T < 1 || p.T > (1 << 30) || p.Hq < 0 || p.Hq > 65535 || p.Hkv < 1 || p.Hkv > 65535 || (D != 64 && D != 128) || p.max_pages < 1 ||
+    if (B < 1 || B > 65535 || p.T < 1 || p.Hq < 0 || p.Hq > 65535 || p.Hkv < 1 || p.Hkv > 65535 || (D != 64 && D != 128) || p.max_pages < 1 ||
         p.max_pages > 262144 || p.R < 0 || p.R > D || p.R % 16 != 0 || (p.R > 0 && p.n_pos < 1) || (interleaved != 0 && interleaved != 1) ||
         p.k_stride < static_cast<int64_t>(p.Hkv) * D || p.v_stride < static_cast<int64_t>(p.Hkv) * D || p.k_stride % align != 0 ||
         p.v_stride % align != 0 || (p.Hq > 0 && (p.q_stride < static_cast<int64_t>(p.Hq) * D || p.q_stride % align != 0)))
         return GRAFT_ERR_SHAPE;
+    const int own = 64 / (D / 8);                              // tokens of a workgroup that does not share one with others
+    if ((static_cast<int64_t>(p.T) + own - 1) / own >= (1ll << 32) / KA_THREADS) return GRAFT_ERR_SHAPE;         // (lanes of a launch)
     if (mx) {
         if (p.page_stride < mx_run_bytes(D) || p.head_stride < mx_run_bytes(D) || p.page_stride % 16 != 0 || p.head_stride % 16 != 0) return GRAFT_ERR_SHAPE;
     } else if (p.page_stride < 1 || p.token_stride < D || p.head_stride < D || p.page_stride % align != 0 || p.token_stride % align != 0 ||
@@ -226,7 +228,7 @@ static int32_t kv_append(AppendParams& p, int32_t B, int32_t D, int32_t interlea
             return GRAFT_ERR_SHAPE;
     }
     const int64_t cus = device_compute_units();
-    const int own = 64 / (D / 8), per = tokens < 3 * own * cus / 4 ? 1 : own;                  // tokens of a workgroup
+    const int per = tokens < 3 * own * cus / 4 ? 1 : own;      // tokens of a workgroup
     const bool share = per == 1;
     // Few tokens' rows go to several workgroups each, as long as there are compute units without one.
     const int64_t steps = (p.Hq + 2 * p.Hkv + KA_THREADS / (D / 8) - 1) / (KA_THREADS / (D / 8)), room = cus / tokens;
