@@ -47,6 +47,7 @@
 //     tree_attn_wide.hip, with the same stages and workspace sizes; the plan and the merge are here.
 //
 // (2) fp32 storage, D = 64, and bf16 with D = 128 where the keys are few: tree_attn_direct.hip.
+#include <atomic>
 #include <cstring>
 
 #include "attn_mfma.h"
@@ -1094,17 +1095,20 @@ struct AttnPlan {
 };
 
 int device_compute_units() {
-    static int cached = 0;
-    if (cached == 0) {
-        int dev = 0, n = 0;
-        if (hipGetDevice(&dev) == hipSuccess &&
-            hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0)
-            cached = n;
-        else
-            cached = 256;
+    static std::atomic<int> known[64];             // of a process's first devices: what was asked once
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess) {
         (void)hipGetLastError();
+        return 256;
     }
-    return cached;
+    const bool kept = dev >= 0 && dev < 64;
+    if (kept && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) {
+        (void)hipGetLastError();
+        return 256;
+    }
+    if (kept) known[dev].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 #ifdef GRAFT_ATTN_STAMPS
@@ -1249,13 +1253,13 @@ static PathChoice make_choice(int32_t B, int32_t K_max, int32_t Hq, int32_t Hkv,
 // to 2.5 us; of a kept choice 0.9).  The reference returned is good until the thread's next call.
 static const PathChoice& choose_path(int32_t B, int32_t K_max, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_pages, int32_t dtype) {
     struct Kept {
-        int32_t key[8];
+        int32_t key[9];
         PathChoice choice;
     };
     constexpr int KEPT = 8;
     static thread_local Kept kept[KEPT]{};
     static thread_local int last = 0, oldest = 0;
-    int32_t key[8] = {B, K_max, Hq, Hkv, D, max_pages, dtype, 1};
+    int32_t key[9] = {B, K_max, Hq, Hkv, D, max_pages, dtype, 1, device_compute_units()};
 #ifdef GRAFT_ATTN_STAMPS
     key[7] += g_force_splits * 8192 + g_force_row_tiles * 2;
 #endif
