@@ -11,7 +11,9 @@
 // With few tokens the lanes of a workgroup share one token's rows, and as long as there are compute units to spare several workgroups do (64 + 2 x 4
 // heads, us: 1 or 48 tokens 5.4 -> 4.2; 384 tokens, with two each, 7.1 -> 7.5).  With so many tokens that three of four compute units get a workgroup all the same, a
 // wavefront's groups of lanes have a token each and its steps are the rows: what it writes to the cache is next to each other, also where elements of tokens are interleaved.
-// (32 + 2 x 8 bf16 heads of 128, us: 512 tokens 6.9 shared and 7.8 not, 1024 tokens 11.5 and 9.0, 16382 tokens 128 and 90.)  Stores do not push
+// (32 + 2 x 8 bf16 heads of 128, us: 512 tokens 6.9 shared and 7.8 not, 1024 tokens 11.5 and 9.0, 16382 tokens 128 and 90.)  The groups are of one
+// sequence: where fewer than half of them would have a token, tokens stay shared.  (Shared and not, us: 1024 x 1 10.0 and 15.0, 4096 x 1 32.6 and 47.7, 2048 x 2
+// 32.5 and 27.8; of heads of 64, which have eight groups, 2048 x 1 10.8 and 24.4, 2730 x 3 32.0 and 35.2, 2048 x 4 31.9 and 28.5.)  Stores do not push
 // what is read out of the caches: 87.  A wait for loads is one for the stores in front of them too, so there 12 rows (8 of float32) are held
 // and not 4: 84.  411 MB in 84 us are 4.9 TB/s.  Fewer rows a workgroup (in more of them) take longer, and so do two batches of rows in turn.
 #include "mx.h"
@@ -228,7 +230,7 @@ static int32_t kv_append(AppendParams& p, int32_t B, int32_t D, int32_t interlea
             return GRAFT_ERR_SHAPE;
     }
     const int64_t cus = device_compute_units();
-    const int per = tokens < 3 * own * cus / 4 ? 1 : own;      // tokens of a workgroup
+    const int per = tokens < 3 * own * cus / 4 || 2 * p.T < own ? 1 : own;                     // tokens of a workgroup, all of one sequence
     const bool share = per == 1;
     // Few tokens' rows go to several workgroups each, as long as there are compute units without one.
     const int64_t steps = (p.Hq + 2 * p.Hkv + KA_THREADS / (D / 8) - 1) / (KA_THREADS / (D / 8)), room = cus / tokens;
