@@ -934,7 +934,7 @@ struct AttnMxPlan {
 //   4 x 96 x 32/8 at 65536  461 / 354     32 x 64 x 32/8 at 4096  149 / 129    16 x 128 x 32/8 at 8192  266 / 229    4 x 64 x 32/8 at 65536  266 / 248
 //   16 x 48 x 32/8 at 8192  113 / 124     16 x 64 x 32/8 at 8192  139 / 143    1 x 128 x 40/8 at 4096    27 / 36     1 x 40 x 32/8 at 2048   15 / 18
 constexpr int TM_MANY = 192;
-static AttnMxPlan plan_attn_mx(int32_t B, int32_t K, int32_t Hq, int32_t Hkv, int32_t max_pages) {
+static AttnMxPlan plan_attn_mx(int32_t B, int32_t K, int32_t Hq, int32_t Hkv, int64_t pages) {          // (that a sequence's nodes may see)
     const int rows = K * (Hq / Hkv), blocks = (rows + 15) / 16;
     AttnMxPlan plan{blocks > 1 ? 2 : 1, TM_WAVES, (blocks + 1) / 2, 1};
     if (rows > TM_MANY && static_cast<int64_t>(B) * Hkv * plan.row_tiles >= device_compute_units()) {
@@ -946,7 +946,7 @@ static AttnMxPlan plan_attn_mx(int32_t B, int32_t K, int32_t Hq, int32_t Hkv, in
     // Two workgroups a compute unit: as many as are at work at a time (with four, us: single tokens of 32 sequences 114 -> 117, of 8 28 -> 35,
     // 64 x 40 rows at 32768 65 -> 72).  A split has at least two tiles of four pages for each wavefront (with one: 64 rows of 8 heads at 256 tokens 10.2 -> 12.2,
     // at 2048 14.3 -> 14.6, at 8192 20.7 -> 22.9; with four: at 2048 19.0 -> 19.8).
-    const int64_t fill = 2 * device_compute_units(), most = (max_pages + 31) / 32;
+    const int64_t fill = 2 * device_compute_units(), most = (pages + 31) / 32;
     int64_t s = groups >= fill ? 1 : fill / groups;
     if (s > most) s = most;
     if (s > TM_MAX_SPLITS) s = TM_MAX_SPLITS;
@@ -988,7 +988,11 @@ extern "C" int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const 
     if (!(factor - factor == 0.0f) || !(softcap >= 0.0f && softcap <= 1024.0f)) return GRAFT_ERR_SHAPE;
     if ((reinterpret_cast<size_t>(q) | reinterpret_cast<size_t>(k_cache) | reinterpret_cast<size_t>(v_cache) | reinterpret_cast<size_t>(out)) & 15)
         return GRAFT_ERR_SHAPE;
-    const AttnMxPlan plan = plan_attn_mx(B, K_max, Hq, Hkv, max_pages);
+    // With a window the keys are split by the pages that it leaves of the table's (nodes' positions are at most K_max apart, or more is left out of
+    // the plan, not of the sums): never into more pieces than without, for which the workspace was asked for.  (One token, 8 heads, a
+    // table of 4064 pages, us: a window of 4096 17.6 by the table and 11.3 by the window, of 128 17.3 and 7.0; 40 nodes, of 1024 17.2 and 14.4.)
+    const int64_t windowed = window / GRAFT_PAGE_SIZE + K_max / GRAFT_PAGE_SIZE + 3, pages = window > 0 && windowed < max_pages ? windowed : max_pages;
+    const AttnMxPlan plan = plan_attn_mx(B, K_max, Hq, Hkv, pages);
     const size_t need = attn_mx_bytes(plan, B, K_max, Hq, D);
     if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<size_t>(workspace) & 15))) return GRAFT_ERR_WORKSPACE;
     AttnMxParams p{};
@@ -1010,7 +1014,6 @@ extern "C" int32_t graft_tree_attn_mx(const void* q, const void* k_cache, const 
     // One tile of rows reads every page once: from more than the Infinity Cache holds on, of the pages that there is room for and that windows leave,
     // loads are nontemporal (us: single tokens of 32 sequences of 16384, 571 MB, 114 -> 106; of 64 of 4096, 286 MB, 47 -> 46; of 8 of 8192,
     // 71 MB, they would be 19 -> 21).
-    const int64_t windowed = window / GRAFT_PAGE_SIZE + K_max / GRAFT_PAGE_SIZE + 3, pages = window > 0 && windowed < max_pages ? windowed : max_pages;
     const bool stream_cache = plan.row_blocks != 0 && plan.row_tiles == 1 && 2 * pages * B * Hkv * mx_run_bytes(D) > TM_CACHED;
     const dim3 blocks(8 * plan.row_tiles, (p.items + 7) / 8);
     auto launch = [&](auto kernel) {
