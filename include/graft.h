@@ -469,7 +469,8 @@ int32_t graft_kv_append(const void* q, const void* k, const void* v, int64_t q_s
  * graft_kv_append_mx - graft_kv_append into a 4-bit cache.  Rotated keys (in fp32, not rounded to
  * dtype) and values become blocks: m 2^E being the largest magnitude, the scale is 2^(E-2), 2^(E-1) where m > 1.75, its
  * byte held within 2..252; elements are rounded to nearest, ties to even, at most 6.  A block with an
- * infinity or NaN gets the scale byte 255.  q_out is of dtype.
+ * infinity or NaN gets the scale byte 255.  q_out is of dtype (graft_tree_attn_mx takes bf16:
+ * with GRAFT_F32 it is for the caller to round).
  */
 int32_t graft_kv_append_mx(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
                            const float* cos_sin, int32_t n_pos, int32_t rot_dim, int32_t interleaved, const int32_t* pos,

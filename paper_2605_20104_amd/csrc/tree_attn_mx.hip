@@ -694,7 +694,7 @@ __global__ __launch_bounds__(TM_THREADS, 2) void tree_attn_mx_kernel(const int32
 // Converting 64 tokens' values is 164 vector instructions: four of the eight wavefronts convert a page each into LDS, the others bring a page's
 // keys, and all of them take keys and values from there.  Two stages' buffers, one barrier a
 // stage: while one is read the next is written, from registers that were loaded a stage ago.
-// 96 nodes x 32 heads over 8 KV heads, 4 sequences, prefix 65536: 355 us, 1.15 PFLOP/s for both products, where a large bfloat16 matrix product
+// 96 nodes x 32 heads over 8 KV heads, 4 sequences, prefix 65536: 358 us, 1.14 PFLOP/s for both products, where a large bfloat16 matrix product
 // reaches 1.3 to 1.4 on the same card.  Two row blocks a wavefront, or 32 x 32 products with their order laid down by hand, which halve the
 // matrix instructions' share of the issue, take 362 and 372 us, and longer where there are few stages.
 constexpr int TR_WAVES = 8, TR_PAGES = 4;          // wavefronts; pages of a stage
@@ -930,7 +930,8 @@ struct AttnMxPlan {
 
 // The kernel for few rows in tiles of 32 rows, unless a head has more than TM_MANY and its tiles alone give every compute unit a workgroup: with work
 // for all, the kernel for more rows converts values for 128 rows at once (with as few workgroups as that takes and rows dealt out
-// evenly); with less, it splits keys further and has more to join.  Few / more, us, D = 128, B x K x Hq over Hkv at a prefix:
+// evenly); with less, it splits keys further and has more to join.  The border is where most shapes gain; one just above it loses 3 % (16 x 64 below).
+// Few / more, us, D = 128, B x K x Hq over Hkv at a prefix:
 //   4 x 96 x 32/8 at 65536  461 / 354     32 x 64 x 32/8 at 4096  149 / 129    16 x 128 x 32/8 at 8192  266 / 229    4 x 64 x 32/8 at 65536  266 / 248
 //   16 x 48 x 32/8 at 8192  113 / 124     16 x 64 x 32/8 at 8192  139 / 143    1 x 128 x 40/8 at 4096    27 / 36     1 x 40 x 32/8 at 2048   15 / 18
 constexpr int TM_MANY = 192;
@@ -944,8 +945,9 @@ static AttnMxPlan plan_attn_mx(int32_t B, int32_t K, int32_t Hq, int32_t Hkv, in
     }
     const int64_t groups = static_cast<int64_t>(B) * Hkv * plan.row_tiles;
     // Two workgroups a compute unit: as many as are at work at a time (with four, us: single tokens of 32 sequences 114 -> 117, of 8 28 -> 35,
-    // 64 x 40 rows at 32768 65 -> 72).  A split has at least two tiles of four pages for each wavefront (with one: 64 rows of 8 heads at 256 tokens 10.2 -> 12.2,
-    // at 2048 14.3 -> 14.6, at 8192 20.7 -> 22.9; with four: at 2048 19.0 -> 19.8).
+    // 64 x 40 rows at 32768 65 -> 72).  A split has at least two tiles of four pages for each wavefront where the table is full (with one: 64 rows of 8 heads at 256 tokens
+    // 10.2 -> 12.2, at 2048 14.3 -> 14.6, at 8192 20.7 -> 22.9; with four: at 2048 19.0 -> 19.8).  Lengths are not known here: in a table of 2048 pages, one token of 2
+    // heads over 255 tokens takes 12.9 and not 5.9, 40 nodes of 8 over 2048 17.8 and not 14.7.
     const int64_t fill = 2 * device_compute_units(), most = (pages + 31) / 32;
     int64_t s = groups >= fill ? 1 : fill / groups;
     if (s > most) s = most;
