@@ -1247,7 +1247,7 @@ static PathChoice make_choice(int32_t B, int32_t K_max, int32_t Hq, int32_t Hkv,
     return c;
 }
 
-// The choices of the last eight shapes are kept per host thread: all layers of a model ask for the same one, a
+// The choices of the last eight shapes (and counts of compute units) are kept per host thread: all layers of a model ask for the same one, a
 // draft and a target model or two batch sizes take turns, and working the cost models out takes one to two
 // microseconds, a sixth of a small launch (workspace query through ctypes, three shapes with a new table size each time: 2.0
 // to 2.5 us; of a kept choice 0.9).  The reference returned is good until the thread's next call.
