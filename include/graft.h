@@ -27,6 +27,12 @@
  *     graft_kv_compact_mx    its update after acceptance
  *     graft_kv_gather_mx     its rows as numbers
  *
+ * and what a request needs before its first tree and behind every one:
+ *
+ *     graft_prompt_attn      attention of a prompt, or of a piece of one, over the paged cache
+ *     graft_token_counts     how often the sequences' contexts hold each token
+ *     graft_logits_adjust    penalties, biases and grammar masks on the nodes' logits, and the greedy tokens that they leave
+ *
  * Conventions shared by every call
  *  - All tensor pointers are DEVICE pointers owned by the caller.  The library
  *    never allocates, frees or keeps them.  Scratch memory comes from
@@ -531,6 +537,84 @@ int32_t graft_kv_compact_mx(void* k_cache, void* v_cache, int64_t layer_stride, 
                             int64_t head_stride, const int32_t* block_table, int32_t max_pages, const int32_t* prefix_len,
                             const int32_t* path, const int32_t* accept_len, int32_t B, int32_t depth_cap, int32_t K_max, int32_t Hkv,
                             int32_t D, int32_t* new_prefix_len, int32_t* status, void* stream);
+
+/*
+ * graft_prompt_attn - causal attention of new tokens over the paged cache that holds what came before them and, appended by
+ * graft_kv_append, themselves: a prompt, a piece of one, single tokens.  One call = one layer.  Token i < n_nodes[b] of sequence b has
+ * position P + i, P = prefix_len[b]; query head h (KV head g = h / (Hq/Hkv)), with x_t = scale * q[b,i,h,:] . k_t[g,:]:
+ *     S   = {tokens t : t <= P + i, and with window > 0 only t > P + i - window}
+ *     out[b,i,h,:] = sum_{t in S} softmax_t(y_t) v_t[g,:],   y_t = softcap > 0 ? softcap tanh(x_t / softcap) : x_t
+ *
+ *     q, out [B,T,Hq,D]   dtype elements, dense; out may be q itself and overlaps nothing else
+ *     caches, strides, block_table, prefix_len   as in graft_tree_attn
+ *     n_nodes [B]         0 <= n_nodes[b] <= T: lengths of a padded batch
+ * Rows of padding tokens are zeros, and so are all rows of a sequence whose prefix_len < 0, n_nodes is outside [0,T] or tokens exceed
+ * the block table.  T is not bounded by GRAFT_MAX_NODES.  What a token does not see, an infinity or NaN of its keys or
+ * values among it, does not reach the token's rows.
+ * dtype GRAFT_BF16: fp32 scores, softmax and sums, probabilities (up to 2^8, relative to a reference of the row) rounded to bf16 for the
+ * second product; GRAFT_F32: fp32 throughout.  A capped score is off by up to 2^-20 of the cap.  Values past 2^100 may overflow in sums.
+ *
+ * workspace: at least graft_prompt_attn_workspace_bytes(...) bytes (0: NULL will do), 16-byte aligned, scratch; calls that may run at
+ * the same time need one each.  It depends on the current device, as graft_tree_attn_workspace_bytes does.
+ *
+ * Requires D in {64,128}, Hq % Hkv == 0, Hq/Hkv <= 16, 1 <= T <= 2^22, 1 <= max_pages <= 262144, B <= 65535, B * Hkv <= 2^18,
+ * B * Hkv * ceil(T (Hq/Hkv) / 128) < 2^23, strides that are multiples of 8 elements, token_stride and head_stride at least D, token_stride < 2^26,
+ * window >= 0, 0 <= softcap <= 1024, 1.45 scale, with a cap 2.9 scale / softcap, finite in fp32, q, out and caches 16-byte aligned.
+ */
+size_t graft_prompt_attn_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_pages, int32_t window,
+                                         int32_t dtype);
+
+int32_t graft_prompt_attn(const void* q, const void* k_cache, const void* v_cache, int64_t page_stride, int64_t token_stride,
+                          int64_t head_stride, const int32_t* block_table, int32_t max_pages, const int32_t* prefix_len,
+                          const int32_t* n_nodes, int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t page_size, float scale,
+                          float softcap, int32_t window, int32_t dtype, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * graft_token_counts - the numbers that penalties go by.  For token t of ctx[b,0..ctx_len[b]):
+ *     t <  prompt_len[b] (prompt_len == NULL: none)   bit 31 of counts[b,ctx[b,t]] is set: the prompt holds it
+ *     t >= prompt_len[b]                              counts[b,ctx[b,t]] grows by one: it was generated
+ * start == NULL: the rows of counts are written anew, zeros where nothing occurs.  Otherwise only the tokens from start[b] on are
+ * added to what counts holds (a round's tokens, in the context buffer or as graft_accept writes them: entries outside [0,V), as its -1
+ * padding, are skipped).
+ *
+ *     ctx [B,L_max], ctx_len [B], prompt_len [B] or NULL, start [B] or NULL, counts [B,V] IN/OUT
+ * status [B]: GRAFT_STATUS_BAD_LENGTH if ctx_len is outside [0,L_max] or start outside [0,ctx_len]; then nothing is counted (the row is
+ * zeros, or with start as it was).  counts overlaps none of the inputs.
+ *
+ * 1 <= B <= 65535, 1 <= L_max < 2^30, V >= 1.
+ */
+int32_t graft_token_counts(const int32_t* ctx, const int32_t* ctx_len, const int32_t* prompt_len, const int32_t* start, int32_t B,
+                           int32_t L_max, int32_t V, int32_t* counts, int32_t* status, void* stream);
+
+/*
+ * graft_logits_adjust - a request's rules on the logits of its tree's nodes, between the target model and graft_accept.  Row i < n_nodes[b] of
+ * sequence b scores what follows node i; its history is what counts says (the context up to and with the root) and the nodes
+ * below the root on its path.  For token v, with c = counts[b,v] (counts == NULL: 0) as graft_token_counts writes it,
+ *     gen = (c & 0x7fffffff) + number of nodes j != 0, bit j of mask[b,i] set, with tokens[b,j] == v,   seen = (bit 31 of c) or gen > 0
+ *     x = logits[b,i,v];   seen:    x = x > 0 ? x / repetition[b] : x * repetition[b]
+ *                          gen > 0: x = x - gen * frequency[b];  x = x - presence[b]
+ *     x = x + bias[v] (or bias[b,v]);   bit v of allow's row allow_index[b,i] clear: x = -infinity
+ * each operation rounded to fp32 by itself, what is not given left out.
+ *
+ *     logits, out [B,K_max,V] fp32   out may be logits itself (in place) or NULL; it overlaps nothing else
+ *     target_ids [B,K_max]           OUT, or NULL: index of the first maximum of the row's x, -1 where every x is -infinity (a
+ *                                    grammar that allows nothing) and for padding nodes; NaN is passed over.  What graft_accept takes
+ *     tokens [B,K_max], mask [B,K_max,GRAFT_MASK_WORDS]   both or neither (no paths: every history is the context)
+ *     repetition, frequency, presence [B], bias [bias_rows,V] with bias_rows 1 or B   each may be NULL
+ *     allow [n_allow,ceil(V/32)]     bit v % 32 of word v / 32; allow_index [B,K_max]: -1 = every token; both or neither
+ * Rows of padding nodes in out are left as they were.  status [B]: GRAFT_STATUS_BAD_TREE if n_nodes is outside [1,K_max] (then out is left and
+ * target_ids are -1), GRAFT_STATUS_BAD_LENGTH if an allow_index is outside [-1,n_allow) (such a row allows nothing).
+ *
+ * 1 <= B <= 65535, 1 <= K_max <= GRAFT_MAX_NODES, V >= 1; with target_ids workspace >= graft_logits_adjust_workspace_bytes(B,K_max,V), 8-byte
+ * aligned, scratch.
+ */
+size_t graft_logits_adjust_workspace_bytes(int32_t B, int32_t K_max, int32_t V);
+
+int32_t graft_logits_adjust(const float* logits, const int32_t* n_nodes, const int32_t* tokens, const uint64_t* mask, int32_t B,
+                            int32_t K_max, int32_t V, const int32_t* counts, const float* repetition, const float* frequency,
+                            const float* presence, const float* bias, int32_t bias_rows, const uint32_t* allow, int32_t n_allow,
+                            const int32_t* allow_index, float* out, int32_t* target_ids, int32_t* status, void* workspace,
+                            size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

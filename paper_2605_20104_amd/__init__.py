@@ -63,6 +63,11 @@ _SIGNATURES = {
     "graft_kv_gather_mx": (_i32, [_vp, _vp, _i64, _i32, _i64, _i64, _vp, _i32, _vp, _vp] + [_i32] * 5 + [_vp] * 4),
     "graft_tree_attn_mx_workspace_bytes": (_sz, [_i32] * 6),
     "graft_tree_attn_mx": (_i32, [_vp] * 3 + [_i64, _i64, _vp, _i32, _vp, _vp, _vp, _vp] + [_i32] * 6 + [_f32, _f32, _i32, _vp, _vp, _sz, _vp]),
+    "graft_prompt_attn_workspace_bytes": (_sz, [_i32] * 8),
+    "graft_prompt_attn": (_i32, [_vp] * 3 + [_i64] * 3 + [_vp, _i32, _vp, _vp] + [_i32] * 6 + [_f32, _f32, _i32, _i32, _vp, _vp, _sz, _vp]),
+    "graft_token_counts": (_i32, [_vp] * 4 + [_i32] * 3 + [_vp] * 3),
+    "graft_logits_adjust_workspace_bytes": (_sz, [_i32] * 3),
+    "graft_logits_adjust": (_i32, [_vp] * 4 + [_i32] * 3 + [_vp] * 5 + [_i32, _vp, _i32] + [_vp] * 5 + [_sz, _vp]),
     "graft_kv_compact_mx": (_i32, [_vp, _vp, _i64, _i32, _i64, _i64, _vp, _i32, _vp, _vp, _vp] + [_i32] * 5 + [_vp] * 3),
 }
 EXPORTED_SYMBOLS = tuple(_SIGNATURES)
@@ -244,3 +249,38 @@ def graft_kv_compact_mx(k_cache, v_cache, layer_stride: int, n_layers: int, stri
     """graft_kv_compact for a 4-bit cache.  Returns dict(new_prefix_len [B], status [B])."""
     return _calls().kv_compact_mx(k_cache, v_cache, layer_stride, n_layers, strides, block_table, prefix_len, path, accept_len, K_max, Hkv, D,
                                  out, stream)
+
+
+def graft_prompt_attn_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int, max_pages: int, window: int, dtype: int) -> int:
+    return int(load_library().graft_prompt_attn_workspace_bytes(B, T, Hq, Hkv, D, max_pages, window, dtype))
+
+
+def graft_prompt_attn(q, k_cache, v_cache, strides, block_table, prefix_len, n_nodes, Hkv: int, scale: float, softcap: float = 0.0,
+                      window: int = 0, out=None, workspace=None, stream=None):
+    """Causal attention of new tokens (a prompt, a piece of one, single tokens) over the paged cache that holds them and what came
+    before, one layer.  q [B,T,Hq,D] float32 or bfloat16 on the GPU, as graft_kv_append returns it; token i < n_nodes[b] has
+    position prefix_len[b] + i.  softcap: scores become softcap tanh(score / softcap); window: a token sees the last `window` positions."""
+    return _calls().prompt_attn(q, k_cache, v_cache, strides, block_table, prefix_len, n_nodes, Hkv, scale, softcap, window, out, workspace,
+                                stream)
+
+
+def graft_token_counts(ctx, ctx_len, prompt_len, counts, start=None, status=None, stream=None):
+    """Occurrences of each token in ctx int32 [B,L_max], into counts int32 [B,V] (updated in place): the top bit of an entry says that
+    the token is among the first prompt_len[b], the bits below how often it occurs later.  start None: rows are written anew; otherwise the
+    tokens from start[b] on are added.  Returns status [B]."""
+    return _calls().token_counts(ctx, ctx_len, prompt_len, counts, start, status, stream)
+
+
+def graft_logits_adjust_workspace_bytes(B: int, K_max: int, V: int) -> int:
+    return int(load_library().graft_logits_adjust_workspace_bytes(B, K_max, V))
+
+
+def graft_logits_adjust(logits, n_nodes, tokens=None, mask=None, counts=None, repetition=None, frequency=None, presence=None, bias=None,
+                        allow=None, allow_index=None, result=None, out=None, workspace=None, stream=None):
+    """Penalties, biases and grammar masks on the logits float32 [B,K,V] of a tree's nodes.  Returns dict(target_ids [B,K],
+    status [B]): the greedy token of each node under the rules, -1 where they allow nothing.  result: a tensor that receives the adjusted
+    logits, `logits` itself for in place.  counts int32 [B,V] from graft_token_counts; tokens [B,K] and mask [B,K,2] add a node's
+    path to its history; repetition, frequency, presence float32 [B]; bias float32 [V] or [B,V]; allow int32 [n,ceil(V/32)] rows of
+    bits, allow_index [B,K] the row of each node (-1: every token)."""
+    return _calls().logits_adjust(logits, n_nodes, tokens, mask, counts, repetition, frequency, presence, bias, allow, allow_index, result, out,
+                                  workspace, stream)

@@ -17,7 +17,8 @@ OBJ_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgraft.so")
 LIB_TIMING = os.path.join(PKG, "libgraft_timing.so")     # the same library with the attention kernel's time stamps
 NATIVE = os.path.join(PKG, "_native.so")                 # tensor marshalling of the Python binding (csrc/binding.cpp)
-SOURCES = ["api.hip", "retrieve.hip", "tree_mask.hip", "tree_attn.hip", "tree_attn_wide.hip", "tree_attn_wide_128.hip", "tree_attn_direct.hip", "tree_attn_parts.hip", "accept.hip", "matrix.hip", "kv_compact.hip", "prune.hip", "kv_append.hip", "kv_mx.hip", "tree_attn_mx.hip"]
+SOURCES = ["api.hip", "retrieve.hip", "tree_mask.hip", "tree_attn.hip", "tree_attn_wide.hip", "tree_attn_wide_128.hip", "tree_attn_direct.hip", "tree_attn_parts.hip", "accept.hip", "matrix.hip", "kv_compact.hip", "prune.hip", "kv_append.hip", "kv_mx.hip", "tree_attn_mx.hip",
+           "prompt_attn.hip", "prompt_attn_bf16.hip", "prompt_attn_f32.hip", "token_counts.hip", "logits_adjust.hip"]
 
 # packed-fp32 code generation is switched off for every device compile; VGPR spills must not
 # land in AccVGPRs (the attention kernel manages those by hand).  Kernel arguments: the first 14 words arrive in
@@ -38,7 +39,7 @@ def _hipcc() -> str:
 
 
 HAND_SCHEDULED = ["tree_attn.hip", "tree_attn_wide.hip", "tree_attn_wide_128.hip", "tree_attn_parts.hip"]
-CHECKED = HAND_SCHEDULED + ["tree_attn_mx.hip"]          # their device assembly is kept and checked
+CHECKED = HAND_SCHEDULED + ["tree_attn_mx.hip", "prompt_attn_bf16.hip"]          # their device assembly is kept and checked
 
 
 def _asm_of(src: str, directory: str = OBJ_DIR) -> str:
@@ -77,8 +78,12 @@ def _reg_span(tok: str):
 
 
 def _managed_accvgprs(symbol: str) -> int:
-    """AccVGPRs that a kernel manages by hand: tree_attn_mfma_kernel<MB>, tree_attn_wide_kernel<NB, MODE> or tree_attn_wide_128_kernel<NB, MODE>;
-    None for others."""
+    """AccVGPRs that a kernel manages by hand: tree_attn_mfma_kernel<MB>, tree_attn_wide_kernel<NB, MODE>, tree_attn_wide_128_kernel<NB, MODE> or
+    prompt_attn_kernel<D, NB, CAP>; None for others."""
+    m = re.match(r"_ZN5graft18prompt_attn_kernelILi(\d+)ELi(\d+)E", symbol)
+    if m:
+        d, nb = int(m.group(1)), int(m.group(2))
+        return nb * (d // 2 + d // 4)
     m = re.match(r"_ZN5graft21tree_attn_mfma_kernelILi(\d+)E", symbol)
     if m:
         mb = int(m.group(1))
@@ -417,7 +422,7 @@ def _check_and_clean(directory: str, what: str, sources):
             raise RuntimeError("%s%s: the generated assembly breaks a rule of the hand-scheduled kernels:\n  "
                                % (src, what) + "\n  ".join(problems[:20]))
     for name in os.listdir(directory):           # the other intermediate files are not needed
-        if name.startswith("tree_attn") and not name.endswith((".o", "gfx950.s")) or name.endswith(".hipfb"):
+        if name.startswith(("tree_attn", "prompt_attn")) and not name.endswith((".o", "gfx950.s")) or name.endswith(".hipfb"):
             os.remove(os.path.join(directory, name))
 
 

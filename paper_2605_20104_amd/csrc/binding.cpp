@@ -30,7 +30,8 @@ namespace {
     X(graft_accept_workspace_bytes) X(graft_accept) X(graft_accept_noalloc) X(graft_matrix_retrieve) \
     X(graft_matrix_update_workspace_bytes) X(graft_matrix_update) X(graft_kv_compact) X(graft_prune_select) \
     X(graft_kv_append) X(graft_kv_append_mx) X(graft_kv_gather_mx) X(graft_tree_attn_mx_workspace_bytes) X(graft_tree_attn_mx) \
-    X(graft_kv_compact_mx) X(graft_last_hip_error)
+    X(graft_kv_compact_mx) X(graft_prompt_attn_workspace_bytes) X(graft_prompt_attn) X(graft_token_counts) \
+    X(graft_logits_adjust_workspace_bytes) X(graft_logits_adjust) X(graft_last_hip_error)
 struct Library {
 #define X(name) decltype(&::name) name = nullptr;
     GRAFT_ENTRY_POINTS(X)
@@ -812,6 +813,150 @@ GRAFT_PY(py_kv_compact_mx, 14) {
     return out.release();
 }
 
+// ---- prompts, and rules on logits -------------------------------------------------------------------
+// q, k_cache, v_cache, strides, block_table, prefix_len, n_nodes, Hkv, scale, softcap, window, out, workspace, stream
+GRAFT_PY(py_prompt_attn, 14) {
+    const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]), &table = tensor(a[4]);
+    const OnDevice on(q);
+    if (q.dim() != 4) {
+        PyErr_Format(PyExc_ValueError, "expected a query tensor of 4 dimensions, got %d", static_cast<int>(q.dim()));
+        throw PythonError();
+    }
+    const at::ScalarType type = q.scalar_type();
+    if ((type != at::kFloat && type != at::kBFloat16) || k.scalar_type() != type || v.scalar_type() != type)
+        fail(PyExc_AssertionError, "queries, keys and values are all float32 or all bfloat16");
+    on.same(k);
+    on.same(v);
+    const int32_t B = size_at(q, 0), T = size_at(q, 1), Hq = size_at(q, 2), D = size_at(q, 3), Hkv = whole(a[7]), window = whole(a[10]);
+    const void *qp = ptr<void>(q), *kp = ptr<void>(k), *vp = ptr<void>(v);
+    const Strides st = strides_of(a[3]);
+    int32_t table_B, max_pages;
+    sizes2(table, table_B, max_pages);
+    const int32_t* pages = on.dense<int32_t>(a[4], {B, max_pages}, at::kInt, "block_table");
+    const int32_t *pl = on.dense<int32_t>(a[5], {B}, at::kInt, "prefix_len"), *n = on.dense<int32_t>(a[6], {B}, at::kInt, "n_nodes");
+    const double scale = PyFloat_AsDouble(a[8]);
+    if (scale == -1.0 && PyErr_Occurred()) throw PythonError();
+    const double cap = PyFloat_AsDouble(a[9]);
+    if (cap == -1.0 && PyErr_Occurred()) throw PythonError();
+    on.gpu();
+    const c10::DeviceGuard guard(on.dev);
+    const LaunchStream stream(a[13], on.dev);
+    const int32_t dtype = type == at::kFloat ? GRAFT_F32 : GRAFT_BF16;
+    at::Tensor new_out, new_ws;
+    void* out;
+    if (a[11] == Py_None) {
+        new_out = empty(q.sizes(), type, on.dev);
+        out = new_out.data_ptr();
+    } else out = on.dense<void>(a[11], q.sizes(), type, "out");
+    void* ws = nullptr;
+    size_t ws_bytes = 0;
+    if (a[12] == Py_None) {
+        ws_bytes = lib.graft_prompt_attn_workspace_bytes(B, T, Hq, Hkv, D, max_pages, window, dtype);
+        if (ws_bytes > 0) {
+            new_ws = stream.scratch(ws_bytes);
+            ws = new_ws.data_ptr();
+        }
+    } else {
+        const at::Tensor& w = tensor(a[12]);
+        on.same(w);
+        ws = ptr<void>(w);
+        ws_bytes = w.nbytes();
+    }
+    void* s = stream.handle();
+    check("graft_prompt_attn", unlocked([&] {
+        return lib.graft_prompt_attn(qp, kp, vp, st.page, st.token, st.head, pages, max_pages, pl, n, B, T, Hq, Hkv, D, GRAFT_PAGE_SIZE,
+                                     static_cast<float>(scale), static_cast<float>(cap), window, dtype, out, ws, ws_bytes, s);
+    }));
+    if (new_out.defined()) return THPVariable_Wrap(std::move(new_out));
+    Py_INCREF(a[11]);
+    return a[11];
+}
+
+// ctx, ctx_len, prompt_len, counts, start, status, stream
+GRAFT_PY(py_token_counts, 7) {
+    const at::Tensor &ctx = tensor(a[0]), &counts = tensor(a[3]);
+    const OnDevice on(ctx);
+    int32_t B, L_max, counts_B, V;
+    sizes2(ctx, B, L_max);
+    sizes2(counts, counts_B, V);
+    const int32_t* c = on.dense<int32_t>(a[0], {B, L_max}, at::kInt, "ctx");
+    int32_t* to = on.dense<int32_t>(a[3], {B, V}, at::kInt, "counts");
+    const int32_t *len = on.dense<int32_t>(a[1], {B}, at::kInt, "ctx_len"), *prompt = on.dense<int32_t>(a[2], {B}, at::kInt, "prompt_len", true),
+                  *start = on.dense<int32_t>(a[4], {B}, at::kInt, "start", true);
+    on.gpu();
+    const c10::DeviceGuard guard(on.dev);
+    const LaunchStream stream(a[6], on.dev);
+    at::Tensor fresh;
+    int32_t* status;
+    if (a[5] == Py_None) {
+        fresh = empty_i32({B}, on.dev);
+        status = static_cast<int32_t*>(fresh.data_ptr());
+    } else status = on.dense<int32_t>(a[5], {B}, at::kInt, "status");
+    void* s = stream.handle();
+    check("graft_token_counts", unlocked([&] { return lib.graft_token_counts(c, len, prompt, start, B, L_max, V, to, status, s); }));
+    if (fresh.defined()) return THPVariable_Wrap(std::move(fresh));
+    Py_INCREF(a[5]);
+    return a[5];
+}
+
+// logits, n_nodes, tokens, mask, counts, repetition, frequency, presence, bias, allow, allow_index, result, out, workspace, stream
+GRAFT_PY(py_logits_adjust, 15) {
+    GRAFT_KEY(target_ids); GRAFT_KEY(status);
+    const at::Tensor& logits = tensor(a[0]);
+    const OnDevice on(logits);
+    if (logits.dim() != 3) {
+        PyErr_Format(PyExc_ValueError, "expected logits of 3 dimensions, got %d", static_cast<int>(logits.dim()));
+        throw PythonError();
+    }
+    const int32_t B = size_at(logits, 0), K = size_at(logits, 1), V = size_at(logits, 2);
+    const float* l = on.dense<float>(a[0], {B, K, V}, at::kFloat, "logits");
+    const int32_t *n = on.dense<int32_t>(a[1], {B}, at::kInt, "n_nodes"), *tokens = on.dense<int32_t>(a[2], {B, K}, at::kInt, "tokens", true),
+                  *counts = on.dense<int32_t>(a[4], {B, V}, at::kInt, "counts", true);
+    const uint64_t* mask = on.dense<uint64_t>(a[3], {B, K, GRAFT_MASK_WORDS}, at::kLong, "mask", true);
+    const float *rep = on.dense<float>(a[5], {B}, at::kFloat, "repetition", true), *freq = on.dense<float>(a[6], {B}, at::kFloat, "frequency", true),
+                *pres = on.dense<float>(a[7], {B}, at::kFloat, "presence", true);
+    const float* bias = nullptr;
+    int32_t bias_rows = 0;
+    if (a[8] != Py_None) {
+        const bool each = tensor(a[8]).dim() == 2;
+        bias = each ? on.dense<float>(a[8], {B, V}, at::kFloat, "bias") : on.dense<float>(a[8], {V}, at::kFloat, "bias");
+        bias_rows = each ? B : 1;
+    }
+    const uint32_t* allow = nullptr;
+    int32_t n_allow = 0;
+    if (a[9] != Py_None) {
+        n_allow = size_at(tensor(a[9]), 0);
+        allow = on.dense<uint32_t>(a[9], {n_allow, (static_cast<int64_t>(V) + 31) / 32}, at::kInt, "allow");
+    }
+    const int32_t* index = on.dense<int32_t>(a[10], {B, K}, at::kInt, "allow_index", true);
+    float* result = on.dense<float>(a[11], {B, K, V}, at::kFloat, "result", true);
+    on.gpu();
+    const c10::DeviceGuard guard(on.dev);
+    const LaunchStream stream(a[14], on.dev);
+    Outputs out(a[12], on.dev);
+    int32_t* ids = out.get_checked(k_target_ids, {B, K});
+    int32_t* status = out.get_checked(k_status, {B});
+    at::Tensor new_ws;
+    void* ws;
+    size_t ws_bytes;
+    if (a[13] == Py_None) {
+        ws_bytes = lib.graft_logits_adjust_workspace_bytes(B, K, V);
+        new_ws = stream.scratch(ws_bytes);
+        ws = new_ws.data_ptr();
+    } else {
+        const at::Tensor& w = tensor(a[13]);
+        on.same(w);
+        ws = ptr<void>(w);
+        ws_bytes = w.nbytes();
+    }
+    void* s = stream.handle();
+    check("graft_logits_adjust", unlocked([&] {
+        return lib.graft_logits_adjust(l, n, tokens, mask, B, K, V, counts, rep, freq, pres, bias, bias_rows, allow, n_allow, index, result, ids, status, ws,
+                                       ws_bytes, s);
+    }));
+    return out.release();
+}
+
 // path of the library, GraftError
 PyObject* py_bind(PyObject*, PyObject* args) {
     const char* path;
@@ -838,7 +983,8 @@ PyMethodDef methods[] = {
     GRAFT_METHOD(retrieve), GRAFT_METHOD(build_tree_mask), GRAFT_METHOD(tree_attn), GRAFT_METHOD(accept),
     GRAFT_METHOD(accept_noalloc), GRAFT_METHOD(matrix_retrieve), GRAFT_METHOD(matrix_update), GRAFT_METHOD(kv_compact),
     GRAFT_METHOD(prune_select), GRAFT_METHOD(kv_append), GRAFT_METHOD(kv_append_mx), GRAFT_METHOD(kv_gather_mx),
-    GRAFT_METHOD(tree_attn_mx), GRAFT_METHOD(kv_compact_mx), {nullptr, nullptr, 0, nullptr}};
+    GRAFT_METHOD(tree_attn_mx), GRAFT_METHOD(kv_compact_mx), GRAFT_METHOD(prompt_attn), GRAFT_METHOD(token_counts),
+    GRAFT_METHOD(logits_adjust), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "Marshalling of the graft_* calls.", -1, methods,
                           nullptr, nullptr, nullptr, nullptr};
 
