@@ -605,7 +605,7 @@ int32_t graft_token_counts(const int32_t* ctx, const int32_t* ctx_len, const int
  * Rows of padding nodes in out are left as they were.  status [B]: GRAFT_STATUS_BAD_TREE if n_nodes is outside [1,K_max] (then out is left and
  * target_ids are -1), GRAFT_STATUS_BAD_LENGTH if an allow_index is outside [-1,n_allow) (such a row allows nothing).
  *
- * 1 <= B <= 65535, 1 <= K_max <= GRAFT_MAX_NODES, V >= 1; with target_ids workspace >= graft_logits_adjust_workspace_bytes(B,K_max,V), 8-byte
+ * 1 <= B <= 65535, 1 <= K_max <= GRAFT_MAX_NODES, 1 <= V < 2^30; with target_ids workspace >= graft_logits_adjust_workspace_bytes(B,K_max,V), 8-byte
  * aligned, scratch.
  */
 size_t graft_logits_adjust_workspace_bytes(int32_t B, int32_t K_max, int32_t V);
