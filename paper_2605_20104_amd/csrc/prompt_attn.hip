@@ -43,24 +43,32 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const int32_t* n_node
     else *reinterpret_cast<floatx4*>(static_cast<float*>(p.out) + to) = sum;
 }
 
-struct PromptPlan { int32_t n_row_tiles, n_splits; size_t o_bytes, bytes; };
-// Splits by what a launch takes, in stages of a row tile: rounds of the compute units times a tile's share of the keys and its set-up, and
-// for splits a launch and the partial rows' way through memory.
+struct PromptPlan { int32_t tile_rows, n_row_tiles, n_splits; size_t o_bytes, bytes; };
+#ifndef PA_FEW
+#define PA_FEW 64
+#endif
+// A kernel and its splits, by what a launch takes: rounds of the compute units times a tile's share of the keys and its set-up, and for splits
+// a launch and the partial rows' way through memory.  The host knows the table's capacity, not the lengths: half of the cost is
+// that of sequences that fill it, half that of ragged ones, three quarters of it in the mean, whose workgroups end one by one.
 static PromptPlan prompt_plan(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_pages, int32_t dtype, int32_t window) {
     const bool f32 = dtype == GRAFT_F32;
-    const int32_t G = Hq / Hkv, tile_rows = f32 ? PA_F32_ROWS : PA_BF16_ROWS, stage = f32 ? 32 : 64;
-    const int64_t R = static_cast<int64_t>(T) * G, tiles = (R + tile_rows - 1) / tile_rows, units = static_cast<int64_t>(B) * Hkv;
-    const int64_t places = static_cast<int64_t>(device_compute_units()) * (f32 ? 2 : 1);
+    const int32_t G = Hq / Hkv;
+    const int64_t R = static_cast<int64_t>(T) * G, units = static_cast<int64_t>(B) * Hkv, cus = device_compute_units();
+    struct Kernel { int32_t rows, stage, per_cu; double stage_us, setup_us; };
+    const Kernel kernel = f32 ? Kernel{PA_F32_ROWS, 32, 2, D == 128 ? 8.0 : 4.0, 3.0}
+                        : R <= 32 ? Kernel{32, 128, 1, D == 128 ? 2.7 : 1.4, 4.0}
+                        : R <= PA_FEW ? Kernel{64, 128, 1, D == 128 ? 2.7 : 1.5, 4.0} : Kernel{PA_BF16_ROWS, 64, D == 128 ? 1 : 2, D == 128 ? 1.2 : 1.4, 4.0};
+    const int64_t tiles = (R + kernel.rows - 1) / kernel.rows, places = cus * kernel.per_cu;
     int64_t keys = static_cast<int64_t>(max_pages) * GRAFT_PAGE_SIZE;
-    const int64_t reach = static_cast<int64_t>(window) + tile_rows / G + 1;
+    const int64_t reach = static_cast<int64_t>(window) + kernel.rows / G + 1;
     if (window > 0 && reach < keys) keys = reach;
-    const int64_t stages = (keys + stage - 1) / stage;
-    const double stage_us = f32 ? (D == 128 ? 8.0 : 4.0) : (D == 128 ? 1.2 : 0.9);
-    PromptPlan best{static_cast<int32_t>(tiles), 1, 0, 0};
+    const int64_t stages = (keys + kernel.stage - 1) / kernel.stage;
+    PromptPlan best{kernel.rows, static_cast<int32_t>(tiles), 1, 0, 0};
     double cost = -1.0;
     for (int64_t s = 1; s <= PA_MAX_SPLITS && s <= stages && tiles * units * s < (1 << 23); ++s) {
-        const double rounds = static_cast<double>((tiles * units * s + places - 1) / places);
-        double now = rounds * (static_cast<double>((stages + s - 1) / s) * stage_us + 3.0);
+        const double jobs = static_cast<double>(tiles * units * s), per = static_cast<double>((stages + s - 1) / s) * kernel.stage_us + kernel.setup_us;
+        const double even = std::ceil(jobs / places) * per, last = 0.75 * jobs / places * per + 0.5 * per, ragged = last > per ? last : per;
+        double now = 0.5 * (even + ragged);
         if (s > 1) now += 4.0 + static_cast<double>(R * units * s) * D * 4 * 2 / 4e6;
         if (cost < 0 || now < cost) { cost = now; best.n_splits = static_cast<int32_t>(s); }
     }
@@ -113,7 +121,9 @@ extern "C" int32_t graft_prompt_attn(const void* q, const void* k_cache, const v
                          token_stride, head_stride, max_pages, B, T, Hq, Hkv, G, T * G, plan.n_splits, plan.n_row_tiles,
                          window > 0 ? window : INT32_MAX, by_g.m, by_g.shift, in, cap_in, softcap * log2e};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const int32_t rc = dtype == GRAFT_F32 ? launch_prompt_f32(p, D, softcap > 0.f, s) : launch_prompt_bf16(p, D, softcap > 0.f, s);
+    const bool cap = softcap > 0.f;
+    const int32_t rc = dtype == GRAFT_F32 ? launch_prompt_f32(p, D, cap, s)
+                     : plan.tile_rows < PA_BF16_ROWS ? launch_prompt_few(p, D, cap, plan.tile_rows, s) : launch_prompt_bf16(p, D, cap, s);
     if (rc != GRAFT_OK || plan.n_splits == 1) return rc;
     auto merge = [&](auto kernel, int rows) { hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>((p.R + rows - 1) / rows) * B * Hkv), dim3(256), 0, s, n_nodes, prefix_len, p); };
     if (dtype == GRAFT_F32) { if (D == 128) merge(prompt_merge_kernel<128, float>, 8); else merge(prompt_merge_kernel<64, float>, 16); }
