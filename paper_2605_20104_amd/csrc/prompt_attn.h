@@ -21,6 +21,7 @@ struct PromptParams {
     int32_t window;         // INT32_MAX: none
     uint32_t g_magic;       // div_any(r, g_magic, g_shift) = r / G
     int32_t g_shift;
+    uint32_t q_sign;        // a negative scale is a positive one with queries of the other sign (hidden scores are -inf, and stay it)
     float scale_log2e;      // scores in log2 units are x * scale_log2e, or
     float cap_in, cap_log2e;    // cap_log2e tanh(x * scale / cap), cap_in = 2 scale log2(e) / cap
 };

@@ -119,7 +119,8 @@ extern "C" int32_t graft_prompt_attn(const void* q, const void* k_cache, const v
     float* const ws = static_cast<float*>(workspace);
     const PromptParams p{q, k_cache, v_cache, out, block_table, prefix_len, n_nodes, ws, plan.bytes ? ws + plan.o_bytes / sizeof(float) : nullptr, page_stride,
                          token_stride, head_stride, max_pages, B, T, Hq, Hkv, G, T * G, plan.n_splits, plan.n_row_tiles,
-                         window > 0 ? window : INT32_MAX, by_g.m, by_g.shift, in, cap_in, softcap * log2e};
+                         window > 0 ? window : INT32_MAX, by_g.m, by_g.shift,
+                         !std::signbit(scale) ? 0u : dtype == GRAFT_F32 ? 0x80000000u : 0x80008000u, std::fabs(in), std::fabs(cap_in), softcap * log2e};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool cap = softcap > 0.f;
     const int32_t rc = dtype == GRAFT_F32 ? launch_prompt_f32(p, D, cap, s)

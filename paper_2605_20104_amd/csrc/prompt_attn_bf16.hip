@@ -16,6 +16,7 @@ namespace graft {
 
 constexpr int PA_STAGE = 64, PA_SUB = 32, PA_NBUF = 4;
 constexpr float PA_RISE = 8.f;                  // log2 units by which scores may pass their row's reference
+constexpr float PA_DAMAGE = 24.f;             // ... and must not, where they are checked late
 constexpr float PA_FRESH = 3e38f;               // minus the reference of a row that has seen nothing
 
 template <int D_, int NB_> struct PromptShape {
@@ -38,7 +39,9 @@ template <class S> struct PromptState {
     uintx4 p[S::NB][2];
     bf16x8 k[S::DK], v[S::DK];
     float l[S::NB], negm[S::NB];
+    float late[S::NB];                          // the largest score past its reference, of units whose check is still to come
     int lim[S::NB];                             // the last token that the lane's row sees
+    bool damaged;
 };
 
 // ---- layout of a stage.  Keys: 16-byte chunk c of row r at c ^ key_swizzle(r); values: 32-byte segment at s ^ value_swizzle(r).
@@ -108,34 +111,49 @@ __device__ __forceinline__ float halves_max(float v) {
     return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// Scores of block B have passed their rows' references (or are the first): new references, what is accumulated scaled down, the
-// probabilities again.
-template <class S, int B> __device__ __forceinline__ void raise_reference(PromptState<S>& w, float c, bool rise, float l_before) {
-    float mm = w.s[B][0] * c;
-#pragma unroll
-    for (int x = 1; x < 16; ++x) mm = __builtin_fmaxf(mm, w.s[B][x] * c);
-    const float negm = rise ? -halves_max(mm) : w.negm[B];
-    const float f = rise ? __builtin_amdgcn_exp2f(negm - w.negm[B]) : 1.f;
-    w.negm[B] = negm;
-    float l = l_before * f;
+// Behind the probabilities of block B's unit, now and then.  Its scores have passed their rows' references (or are the first):
+// new references, what is accumulated scaled down, the probabilities again.  Units without a check of their own: probabilities of up
+// to 2^PA_DAMAGE are accumulated as they are; past that they, and sums and products with them, may not be numbers any more.
+template <class S, int B> __device__ __forceinline__ void raise_reference(PromptState<S>& w, float c, float top, float l_before) {
     GRAFT_MFMA_SETTLE();
-    static_for<0, 16 * S::DE>([&](auto x_) {
-        GRAFT_CONST(x, x_);
-        acc_scale<S::o(B, 0) + x>(f);
+    static_for<0, S::NB>([&](auto b_) {
+        GRAFT_CONST(b, b_);
+        const float late = halves_max(w.late[b]);
+        w.damaged = w.damaged || __builtin_amdgcn_ballot_w64(late > PA_DAMAGE) != 0;
+        float negm = w.negm[b], l = b == B ? l_before : w.l[b];
+        if (late > PA_RISE) negm -= late;
+        if constexpr (b == B) {
+            float mm = w.s[b][0] * c;
+#pragma unroll
+            for (int x = 1; x < 16; ++x) mm = __builtin_fmaxf(mm, w.s[b][x] * c);
+            mm = halves_max(mm);
+            if (mm + negm > PA_RISE) negm = -mm;
+        }
+        const float f = negm < w.negm[b] ? __builtin_amdgcn_exp2f(negm - w.negm[b]) : 1.f;
+        w.negm[b] = negm;
+        w.late[b] = -INFINITY;
+        l *= f;
+        static_for<0, 16 * S::DE>([&](auto x_) {
+            GRAFT_CONST(x, x_);
+            acc_scale<S::o(b, 0) + x>(f);
+        });
+        if constexpr (b == B) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(w.s[b][2 * j], c, negm)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(w.s[b][2 * j + 1], c, negm));
+                l += p0;
+                l += p1;
+                w.p[b][j >> 2][j & 3] = pack_bf16(p0, p1);
+            }
+        }
+        w.l[b] = l;
     });
     GRAFT_MFMA_SETTLE();
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(w.s[B][2 * j], c, negm)), b = __builtin_amdgcn_exp2f(__builtin_fmaf(w.s[B][2 * j + 1], c, negm));
-        l += a;
-        l += b;
-        w.p[B][j >> 2][j & 3] = pack_bf16(a, b);
-    }
-    w.l[B] = l;
 }
 
-// One phase: scores of unit J, probabilities of unit J - 1, products of unit J - 2.
-template <class S, int J, bool QK, bool SM, bool PV, class Extra>
+// One phase: scores of unit J, probabilities of unit J - 1, products of unit J - 2.  CHECK: with the check of the references, a branch, which
+// costs a phase 12 per cent of its time.
+template <class S, int J, bool QK, bool SM, bool PV, bool CHECK, class Extra>
 __device__ __forceinline__ void prompt_phase(PromptState<S>& w, float c, unsigned k_next, unsigned v_next, Extra&& extra) {
     constexpr int QB = S::block(J), SB = S::block(J - 1), PB = S::block(J - 2), PER = 16 / S::SLOTS;
     constexpr bool K_RELOAD = QK && S::last_of_sub(J), V_RELOAD = QK && S::last_of_sub(J - 2);      // for the next 32 tokens
@@ -171,9 +189,12 @@ __device__ __forceinline__ void prompt_phase(PromptState<S>& w, float c, unsigne
         w.l[SB] = in_place(w.l[SB] + e[15]);
     }
     if constexpr (V_RELOAD) w.v[S::DK - 1] = read_values<S>(v_next, S::DK - 1);
-    if constexpr (SM) {
-        const bool rise = halves_max(top) > PA_RISE;
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(rise) != 0, 0)) raise_reference<S, SB>(w, c, rise, l_before);
+    if constexpr (SM && !CHECK) w.late[SB] = in_place(__builtin_fmaxf(w.late[SB], top));
+    if constexpr (SM && CHECK) {
+#pragma unroll
+        for (int b = 0; b < S::NB; ++b) top = __builtin_fmaxf(top, w.late[b]);
+        const bool rise = top > PA_RISE;
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(rise) != 0, 0)) raise_reference<S, SB>(w, c, top, l_before);
     }
     __builtin_amdgcn_sched_barrier(0);
 }
@@ -213,23 +234,31 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
         const int r = r_tile + (wave * NB + rb) * 32 + l32, i = div_any(r, p.g_magic, p.g_shift);
         row_of[rb] = r;
         live[rb] = r < p.R && i < len.n;
-        w.lim[rb] = len.P + i;
-        w.l[rb] = 0.f;
-        w.negm[rb] = PA_FRESH;
+        w.lim[rb] = len.P + (live[rb] ? i : t.i1);                // (rows that are not there see what others see)
         const unsigned short* q = static_cast<const unsigned short*>(p.q) +
             ((static_cast<int64_t>(b) * p.T + i) * p.Hq + g * p.G + (r - i * p.G)) * D + 8 * half;
 #pragma unroll
         for (int d = 0; d < S::DK; ++d) {
             qd[rb][d] = uintx4{0u, 0u, 0u, 0u};
-            if (live[rb]) qd[rb][d] = *reinterpret_cast<const uintx4*>(q + 16 * d);
+            if (live[rb]) qd[rb][d] = *reinterpret_cast<const uintx4*>(q + 16 * d) ^ p.q_sign;
         }
-        w.p[rb][0] = w.p[rb][1] = uintx4{0u, 0u, 0u, 0u};
     }
     reserve_registers<S>();
-    static_for<0, 16 * NB * S::DE>([&](auto x_) {
-        GRAFT_CONST(x, x_);
-        acc_set<x>(0.f);
-    });
+    auto clear_rows = [&]() __attribute__((always_inline)) {
+        static_for<0, 16 * NB * S::DE>([&](auto x_) {
+            GRAFT_CONST(x, x_);
+            acc_set<x>(0.f);
+        });
+#pragma unroll
+        for (int rb = 0; rb < NB; ++rb) {
+            w.l[rb] = 0.f;
+            w.negm[rb] = PA_FRESH;
+            w.late[rb] = -INFINITY;
+            w.p[rb][0] = w.p[rb][1] = uintx4{0u, 0u, 0u, 0u};
+        }
+        w.damaged = false;
+    };
+    clear_rows();
     static_for<0, NB>([&](auto rb_) {
         GRAFT_CONST(rb, rb_);
         static_for<0, 4 * S::DK>([&](auto x_) {
@@ -255,7 +284,7 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
             asm volatile("" : "+v"(x));          // (waited for here, not where it is used, behind transfers)
             return x;
         };
-        int32_t pages = load_table(0);
+        int32_t pages = 0;
         struct PageOf { uintx4 k, v; unsigned lds; };
         auto page_of = [&](int k) __attribute__((always_inline)) {
             PageOf d;
@@ -279,9 +308,6 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
 #pragma unroll
             for (int n = 0; n < S::LOADS; ++n) move(d, n);
         };
-        move_page(0);
-        move_page(1);
-        move_page(2);
         // every stage is LOADS instructions of a wavefront, whatever they move
         auto arrive = [&](auto newer_) __attribute__((always_inline)) {     // all but the newest stages are there, for everybody
             GRAFT_CONST(newer, newer_);
@@ -295,14 +321,6 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
         const unsigned v_lane = kv_base + V_OFF + v_row * RB + (((l32 >> 4) ^ value_swizzle<D>(v_row)) << 5) + 8 * (l16 & 3);
         auto sub_base = [&](int k, int sub) __attribute__((always_inline)) { return static_cast<unsigned>((k & (PA_NBUF - 1)) * S::STAGE_BYTES) + sub * SUB; };
 
-        arrive(std::integral_constant<int, 2>{});
-#pragma unroll
-        for (int d = 0; d < S::DK; ++d) {
-            w.k[d] = read_keys<S>(k_lane + sub_base(0, 0), d);
-            w.v[d] = __builtin_bit_cast(bf16x8, uintx4{0u, 0u, 0u, 0u});
-        }
-#pragma unroll
-        for (int x = 0; x < 16; ++x) w.s[S::block(UNITS - 1)][x] = -INFINITY;
         const float c = CAP ? 1.f : p.scale_log2e;
 
         // Values that are not numbers, in a stage that not every row sees whole: 0 times them would reach rows that do not.
@@ -363,7 +381,7 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
                 constexpr int QB = S::block(J);
                 const unsigned k_next = k_lane + (J == UNITS - 1 ? sub_base(k + 1, 0) : sub_base(k, 1));
                 const unsigned v_next = v_lane + (S::wrap(J - 2) == UNITS - 1 ? sub_base(k, 0) : sub_base(k, 1));
-                prompt_phase<S, J, true, true, true>(w, c, k_next, v_next, [&](auto i_) __attribute__((always_inline)) {
+                prompt_phase<S, J, true, true, true, !PLAIN || J == 0>(w, c, k_next, v_next, [&](auto i_) __attribute__((always_inline)) {
                     GRAFT_CONST(i, i_);
                     constexpr int at = S::SLOTS * J + i, SPACE = S::SLOTS * UNITS / S::LOADS / 2;
                     if constexpr (at == 0) next = page_of(k + 3);
@@ -377,27 +395,50 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
                 if constexpr (!PLAIN) hide<S, QB>(w, (st0 + k) * PA_STAGE + (J / NB) * PA_SUB, half, p.window);
             });
         };
-        // stages that every row of the tile sees whole: plain_from .. plain_to
-        const int low = len.P + t.i1 - p.window, high = len.P + t.i0 + 1;       // tokens behind `low` and in front of `high`
-        int plain_from = low < 0 ? 0 : low / PA_STAGE + 1 - st0, plain_to = high / PA_STAGE - st0;
+        // Stages that every row of the tile sees whole, behind one (the split's first, or the last with a row's first token) that is checked
+        // as it goes, so that every row has its reference: plain_from .. plain_to.
+        const int first = len.P + t.i1 - p.window + 1, whole = first < 0 ? 1 : first / PA_STAGE + 1 - st0;
+        const int plain_from = whole < 1 ? 1 : whole;
+        int plain_to = (len.P + t.i0 + 1) / PA_STAGE - st0;
         plain_to = plain_to < n_st ? plain_to : n_st;
         const auto next_pages = [&](int k) __attribute__((always_inline)) { if (((k + 3) & 63) == 0) pages = load_table(k + 3); };
-        for (int k = 0; k < n_st;) {             // (loops of their own: the registers stay where they are from stage to stage)
-            const int masked_to = k < plain_from ? (plain_from < n_st ? plain_from : n_st) : (k < plain_to ? k : n_st);
-            while (k < masked_to) {
-                stage(k, std::false_type{});
-                next_pages(++k);
+        for (;;) {
+            pages = load_table(0);
+            move_page(0);
+            move_page(1);
+            move_page(2);
+            arrive(std::integral_constant<int, 2>{});
+#pragma unroll
+            for (int d = 0; d < S::DK; ++d) {
+                w.k[d] = read_keys<S>(k_lane + sub_base(0, 0), d);
+                w.v[d] = __builtin_bit_cast(bf16x8, uintx4{0u, 0u, 0u, 0u});
             }
-            while (k < plain_to) {
-                stage(k, std::true_type{});
-                next_pages(++k);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) w.s[S::block(UNITS - 1)][x] = -INFINITY;
+            for (int k = 0; k < n_st;) {         // (loops of their own: the registers stay where they are from stage to stage)
+                const int masked_to = k < plain_from ? (plain_from < n_st ? plain_from : n_st) : (k < plain_to ? k : n_st);
+                while (k < masked_to) {
+                    stage(k, std::false_type{});
+                    next_pages(++k);
+                }
+                while (k < plain_to) {
+                    stage(k, std::true_type{});
+                    next_pages(++k);
+                }
             }
+            const auto nothing = [](auto) {};
+            prompt_phase<S, 0, false, true, true, true>(w, c, 0u, 0u, nothing);
+            prompt_phase<S, 1, false, false, true, false>(w, c, 0u, 0u, nothing);
+            GRAFT_MFMA_SETTLE();
+            GRAFT_WAIT_VMCNT(0);                 // (transfers of stages that are not there)
+            lds_barrier();
+            if (lane == 0) vote[wave] = w.damaged;
+            lds_barrier();
+            if (__builtin_expect((vote[0] | vote[1] | vote[2] | vote[3]) == 0, 1)) break;
+            plain_to = 0;                        // once more, every unit checked
+            clear_rows();
+            GRAFT_MFMA_SETTLE();
         }
-        const auto nothing = [](auto) {};
-        prompt_phase<S, 0, false, true, true>(w, c, 0u, 0u, nothing);
-        prompt_phase<S, 1, false, false, true>(w, c, 0u, 0u, nothing);
-        GRAFT_MFMA_SETTLE();
-        GRAFT_WAIT_VMCNT(0);                     // (transfers of stages that are not there)
     }
     // ---- results: dims 32 e + 8 j + 4 half + 0..3 of row l32 in a[o(rb, e) + 4 j ..]
     static_for<0, NB>([&](auto rb_) {

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void prompt_attn_f32_kernel(const in
 #pragma unroll
         for (int c = 0; c < DC; ++c) {
             q[c] = floatx4{0.f, 0.f, 0.f, 0.f};
-            if (live) q[c] = *reinterpret_cast<const floatx4*>(from + 8 * c);
+            if (live) q[c] = __builtin_bit_cast(floatx4, *reinterpret_cast<const uintx4*>(from + 8 * c) ^ p.q_sign);
         }
     }
     floatx16 o[DE];

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_few_kernel(const int32_t
 #pragma unroll
         for (int d = 0; d < DK; ++d) {
             uintx4 x = {0u, 0u, 0u, 0u};
-            if (live[rb]) x = *reinterpret_cast<const uintx4*>(from + 16 * d);
+            if (live[rb]) x = *reinterpret_cast<const uintx4*>(from + 16 * d) ^ p.q_sign;
             q[rb][d] = __builtin_bit_cast(bf16x8, x);
         }
 #pragma unroll

@@ -40,3 +40,53 @@ CASES = [
 def test_against_64_bits(dtype, B, T, Hq, Hkv, D, P, n, layout, window, cap):
     c = make(B * 7 + T, dtype, B, T, Hq, Hkv, D, P, n, layout)
     check(c, call(c, window, cap), window, cap)
+
+
+# Scores that rise as the keys go on: in steps that references follow, by more than probabilities hold, in one place, in the last stage.
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("T,P", [(1, 900), (300, 700)])
+@pytest.mark.parametrize("kind", ["slow", "steps", "jump", "end", "fall", "negative scale"])
+def test_rising_scores(dtype, D, T, P, kind):
+    c = make(5, dtype, 1, T, 4, 2, D, P)
+    n = P + T
+    t = torch.arange(n, dtype=torch.float64)
+    height = {"slow": t / 40, "steps": (t // 64) * 30, "jump": (t > 500) * 300.0, "end": (t > n - 20) * 200.0, "fall": -t, "negative scale": t / 10}[kind]
+    # the first dim carries the height: q = 1 there, so x = scale * height + noise
+    c["q"][..., 0] = 1.0
+    keys = c["k"].float() * 0.1
+    for s in range(c["pages"]):
+        for o in range(16):
+            if 16 * s + o < n:
+                keys[c["table"][0, s], :, o, 0] = float(height[16 * s + o]) / c["scale"]
+    c["k"] = keys.to(c["k"].dtype)
+    if kind == "negative scale":
+        c["scale"] = -c["scale"]
+    check(c, call(c))
+
+
+# What a token does not see does not reach it, whatever it is.
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,window", [(1, 40), (3, 40), (100, 0), (200, 70), (200, 1)])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_infinities_in_hidden_places(dtype, T, window, bad):
+    P = 150
+    c = make(9, dtype, 1, T, 6, 2, 128, P, T, extra_pages=1)
+    clean = call(c, window).float().cpu()
+    n = P + T
+    at = sorted({10, P + T // 2, n - 1} if T > 3 else {10, 50})
+    for which in "kv":
+        d = dict(c, k=c["k"].clone(), v=c["v"].clone())
+        for t in at:
+            d[which][d["table"][0, t // 16], 1, t % 16, 5] = bad
+        # slots behind the last token, and pages that nobody has
+        d[which][d["table"][0, n // 16], :, n % 16:] = bad
+        got = call(d, window).float().cpu()
+        assert torch.equal(got[:, :, :3], clean[:, :, :3])                     # the other KV head
+        for i in range(T):
+            seen = [t for t in at if t <= P + i and (not window or t > P + i - window)]
+            row = got[0, i, 3:]
+            if not seen:
+                assert torch.equal(row, clean[0, i, 3:]), (which, i)
+            elif which == "v":
+                assert not torch.isfinite(row[:, 5]).any()
+                assert torch.isfinite(torch.cat([row[:, :5], row[:, 6:]], 1)).all()
