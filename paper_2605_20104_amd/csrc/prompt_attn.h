@@ -48,15 +48,19 @@ __device__ __forceinline__ PromptRange prompt_range(const PromptParams& p, Promp
     return t;
 }
 
-// Workgroups, one for each (sequence, KV head, split) = unit and row tile, are dealt to the 8 XCDs as xcd_work_item deals them (row tiles
-// of a unit on one XCD, side by side), for any number of row tiles; the last tiles, which see most keys, come first.
+// Workgroups, one for each (sequence, KV head, split) = unit and row tile, are dealt to the 8 XCDs as xcd_work_item deals them: all
+// row tiles of a unit on one XCD, those of what is left over one by one.  The last tiles, which see most keys, come first, of all
+// of an XCD's units before the next ones of any: unit by unit, the last units' long tiles started when everything else was done (four ragged prompts of
+// 2049, 8 KV heads: 114 -> 97 us).
 struct PromptItem { int unit, row_tile; };                         // unit < 0: padding of the grid
 inline unsigned prompt_grid(const PromptParams& p) { return xcd_grid(static_cast<int64_t>(p.B) * p.Hkv * p.n_splits, p.n_row_tiles); }
 __device__ __forceinline__ PromptItem prompt_item(const PromptParams& p) {
-    const int n_units = p.B * p.Hkv * p.n_splits, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, whole = (n_units >> 3) * p.n_row_tiles;
+    const int n_units = p.B * p.Hkv * p.n_splits, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, each = n_units >> 3, whole = each * p.n_row_tiles;
     const bool left = slot >= whole;
-    const int s = left ? (slot - whole) * 8 + xcd : slot, u = s / p.n_row_tiles, unit = left ? (n_units & ~7) + u : u * 8 + xcd;
-    return {unit < n_units ? unit : -1, p.n_row_tiles - 1 - (s - u * p.n_row_tiles)};
+    const int s = left ? (slot - whole) * 8 + xcd : slot, among = left ? n_units & 7 : each;
+    if (among == 0) return {-1, 0};
+    const int rank = s / among, u = s - rank * among, unit = left ? (n_units & ~7) + u : u * 8 + xcd;
+    return {rank < p.n_row_tiles ? unit : -1, p.n_row_tiles - 1 - rank};
 }
 
 // y of the capped scores in log2 units: cap log2(e) tanh(x scale / cap), as 1 - 2 / (1 + e^2z).  Off by a few 2^-24 of the cap.

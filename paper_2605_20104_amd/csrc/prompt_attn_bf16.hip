@@ -402,7 +402,7 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
         int plain_to = (len.P + t.i0 + 1) / PA_STAGE - st0;
         plain_to = plain_to < n_st ? plain_to : n_st;
         const auto next_pages = [&](int k) __attribute__((always_inline)) { if (((k + 3) & 63) == 0) pages = load_table(k + 3); };
-        for (;;) {
+        for (int attempt = 0;; ++attempt) {
             pages = load_table(0);
             move_page(0);
             move_page(1);
@@ -434,7 +434,7 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
             lds_barrier();
             if (lane == 0) vote[wave] = w.damaged;
             lds_barrier();
-            if (__builtin_expect((vote[0] | vote[1] | vote[2] | vote[3]) == 0, 1)) break;
+            if (__builtin_expect(attempt > 0 || (vote[0] | vote[1] | vote[2] | vote[3]) == 0, 1)) break;
             plain_to = 0;                        // once more, every unit checked
             clear_rows();
             GRAFT_MFMA_SETTLE();
