@@ -111,10 +111,15 @@ __device__ __forceinline__ float halves_max(float v) {
     return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// Scores to log2 units: c x, or with a cap c = cap log2(e) times tanh(x in / 2 log2(e)).
+struct ToLog2 { float c, in; };
+
 // Behind the probabilities of block B's unit, now and then.  Its scores have passed their rows' references (or are the first):
 // new references, what is accumulated scaled down, the probabilities again.  Units without a check of their own: probabilities of up
 // to 2^PA_DAMAGE are accumulated as they are; past that they, and sums and products with them, may not be numbers any more.
-template <class S, int B> __device__ __forceinline__ void raise_reference(PromptState<S>& w, float c, float top, float l_before) {
+// RAW: scores whose cap is still to come.
+template <class S, int B, bool RAW> __device__ __forceinline__ void raise_reference(PromptState<S>& w, ToLog2 to, float l_before) {
+    auto score = [&](int x) __attribute__((always_inline)) { return RAW ? capped(w.s[B][x], to.in, to.c) : w.s[B][x] * to.c; };
     GRAFT_MFMA_SETTLE();
     static_for<0, S::NB>([&](auto b_) {
         GRAFT_CONST(b, b_);
@@ -123,9 +128,9 @@ template <class S, int B> __device__ __forceinline__ void raise_reference(Prompt
         float negm = w.negm[b], l = b == B ? l_before : w.l[b];
         if (late > PA_RISE) negm -= late;
         if constexpr (b == B) {
-            float mm = w.s[b][0] * c;
+            float mm = score(0);
 #pragma unroll
-            for (int x = 1; x < 16; ++x) mm = __builtin_fmaxf(mm, w.s[b][x] * c);
+            for (int x = 1; x < 16; ++x) mm = __builtin_fmaxf(mm, score(x));
             mm = halves_max(mm);
             if (mm + negm > PA_RISE) negm = -mm;
         }
@@ -140,7 +145,8 @@ template <class S, int B> __device__ __forceinline__ void raise_reference(Prompt
         if constexpr (b == B) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(w.s[b][2 * j], c, negm)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(w.s[b][2 * j + 1], c, negm));
+                const float p0 = __builtin_amdgcn_exp2f(RAW ? score(2 * j) + negm : __builtin_fmaf(w.s[b][2 * j], to.c, negm));
+                const float p1 = __builtin_amdgcn_exp2f(RAW ? score(2 * j + 1) + negm : __builtin_fmaf(w.s[b][2 * j + 1], to.c, negm));
                 l += p0;
                 l += p1;
                 w.p[b][j >> 2][j & 3] = pack_bf16(p0, p1);
@@ -151,16 +157,33 @@ template <class S, int B> __device__ __forceinline__ void raise_reference(Prompt
     GRAFT_MFMA_SETTLE();
 }
 
-// One phase: scores of unit J, probabilities of unit J - 1, products of unit J - 2.  CHECK: with the check of the references, a branch, which
-// costs a phase 12 per cent of its time.
-template <class S, int J, bool QK, bool SM, bool PV, bool CHECK, class Extra>
-__device__ __forceinline__ void prompt_phase(PromptState<S>& w, float c, unsigned k_next, unsigned v_next, Extra&& extra) {
+// One phase: scores of unit J, probabilities of unit J - 1 (RAW: their cap on the way), products of unit J - 2.  CHECK: with the check of
+// the references.
+template <class S, int J, bool QK, bool SM, bool PV, bool CHECK, bool RAW, class Extra>
+__device__ __forceinline__ void prompt_phase(PromptState<S>& w, ToLog2 to, unsigned k_next, unsigned v_next, Extra&& extra) {
     constexpr int QB = S::block(J), SB = S::block(J - 1), PB = S::block(J - 2), PER = 16 / S::SLOTS;
     constexpr bool K_RELOAD = QK && S::last_of_sub(J), V_RELOAD = QK && S::last_of_sub(J - 2);      // for the next 32 tokens
-    float y[16], e[16], top = -INFINITY;
+    float t[16], y[16], e[16], top = -INFINITY;
     reserve_registers<S>();
     if constexpr (!QK) asm volatile("s_nop 1");
-    const float l_before = w.l[SB];
+    const float l_before = w.l[SB], base = RAW ? w.negm[SB] + to.c : w.negm[SB];
+    // Element x, in slots of their own where a cap makes it a chain: the exponential of tanh, its reciprocal, then the rest.
+    auto first = [&](auto x_) __attribute__((always_inline)) {
+        GRAFT_CONST(x, x_);
+        t[x] = in_place(__builtin_amdgcn_exp2f(w.s[SB][x] * to.in));
+    };
+    auto second = [&](auto x_) __attribute__((always_inline)) {
+        GRAFT_CONST(x, x_);
+        t[x] = in_place(__builtin_amdgcn_rcpf(1.f + t[x]));
+    };
+    auto last = [&](auto x_) __attribute__((always_inline)) {
+        GRAFT_CONST(x, x_);
+        y[x] = RAW ? __builtin_fmaf(-2.f * to.c, t[x], base) : __builtin_fmaf(w.s[SB][x], to.c, base);
+        e[x] = in_place(__builtin_amdgcn_exp2f(y[x]));
+        if constexpr (x % 2 == 1) top = in_place(__builtin_fmaxf(__builtin_fmaxf(top, y[x - 1]), y[x]));
+        if constexpr (x >= 1) w.l[SB] = in_place(w.l[SB] + e[x - 1]);
+        if constexpr (x >= 2 && x % 2 == 0) w.p[SB][(x - 2) >> 3][((x - 2) >> 1) & 3] = in_place(pack_bf16(e[x - 2], e[x - 1]));
+    };
     static_for<0, S::SLOTS>([&](auto i_) {
         GRAFT_CONST(i, i_);
         constexpr int h = i >> 1;
@@ -169,21 +192,24 @@ __device__ __forceinline__ void prompt_phase(PromptState<S>& w, float c, unsigne
         } else {
             if constexpr (PV) mfma_output<S::o(PB, h % S::DE)>(w.v[h], w.p[PB][h / S::DE]);
         }
-        if constexpr (SM) {
-            static_for<(i < 2 ? 0 : PER * i), (i == 0 ? 0 : PER * (i + 1))>([&](auto x_) {          // (the scores have settled by slot 1)
-                GRAFT_CONST(at, x_);
-                y[at] = __builtin_fmaf(w.s[SB][at], c, w.negm[SB]);
-                e[at] = in_place(__builtin_amdgcn_exp2f(y[at]));
-                if constexpr (at % 2 == 1) top = in_place(__builtin_fmaxf(__builtin_fmaxf(top, y[at - 1]), y[at]));
-                if constexpr (at >= 1) w.l[SB] = in_place(w.l[SB] + e[at - 1]);
-                if constexpr (at >= 2 && at % 2 == 0) w.p[SB][(at - 2) >> 3][((at - 2) >> 1) & 3] = in_place(pack_bf16(e[at - 2], e[at - 1]));
-            });
+        if constexpr (SM) {                      // (the scores have settled by slot 1)
+            constexpr int to1 = i == 0 ? 0 : PER * (i + 1), from1 = i < 2 ? 0 : PER * i;
+            constexpr int to2 = i < 2 ? 0 : PER * i, from2 = i < 3 ? 0 : PER * (i - 1), to3 = i < 3 ? 0 : PER * (i - 1), from3 = i < 4 ? 0 : PER * (i - 2);
+            if constexpr (RAW) {
+                static_for<from1, to1>(first);
+                static_for<from2, to2>(second);
+                static_for<from3, to3>(last);
+            } else static_for<from1, to1>(last);
         }
         if constexpr (K_RELOAD && i % 2 == 1) w.k[h] = read_keys<S>(k_next, h);
         if constexpr (V_RELOAD && i % 2 == 0 && i >= 2) w.v[h - 1] = read_values<S>(v_next, h - 1);
         extra(i_);
         __builtin_amdgcn_sched_barrier(0);
     });
+    if constexpr (SM && RAW) {
+        static_for<16 - PER, 16>(second);
+        static_for<16 - 2 * PER, 16>(last);
+    }
     if constexpr (SM) {
         w.p[SB][1][3] = in_place(pack_bf16(e[14], e[15]));
         w.l[SB] = in_place(w.l[SB] + e[15]);
@@ -193,8 +219,7 @@ __device__ __forceinline__ void prompt_phase(PromptState<S>& w, float c, unsigne
     if constexpr (SM && CHECK) {
 #pragma unroll
         for (int b = 0; b < S::NB; ++b) top = __builtin_fmaxf(top, w.late[b]);
-        const bool rise = top > PA_RISE;
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(rise) != 0, 0)) raise_reference<S, SB>(w, c, top, l_before);
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > PA_RISE) != 0, 0)) raise_reference<S, SB, RAW>(w, to, l_before);
     }
     __builtin_amdgcn_sched_barrier(0);
 }
@@ -321,7 +346,12 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
         const unsigned v_lane = kv_base + V_OFF + v_row * RB + (((l32 >> 4) ^ value_swizzle<D>(v_row)) << 5) + 8 * (l16 & 3);
         auto sub_base = [&](int k, int sub) __attribute__((always_inline)) { return static_cast<unsigned>((k & (PA_NBUF - 1)) * S::STAGE_BYTES) + sub * SUB; };
 
-        const float c = CAP ? 1.f : p.scale_log2e;
+        const ToLog2 done = {CAP ? 1.f : p.scale_log2e, 0.f}, raw = {p.cap_log2e, p.cap_in};
+        auto cap_scores = [&](floatx16& x) __attribute__((always_inline)) {
+            settle_scores(x);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[j] = capped(x[j], p.cap_in, p.cap_log2e);
+        };
 
         // Values that are not numbers, in a stage that not every row sees whole: 0 times them would reach rows that do not.
         // They are added to the rows that see them here, and become zeros.
@@ -371,8 +401,10 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
             lds_barrier();
         };
 
-        auto stage = [&](int k, auto plain_) __attribute__((always_inline)) {
-            constexpr bool PLAIN = decltype(plain_)::value;
+        // Caps: in a PLAIN stage on the way to the probabilities, a phase behind the scores (RAW_BEFORE: those of the stage before wait for
+        // theirs); elsewhere at once, since what is hidden has to stay so.
+        auto stage = [&](int k, auto plain_, auto raw_before_) __attribute__((always_inline)) {
+            constexpr bool PLAIN = decltype(plain_)::value, RAW_BEFORE = decltype(raw_before_)::value;
             PageOf next;
             arrive(std::integral_constant<int, 1>{});              // stage k + 1 is there; nobody reads stage k - 1 any more
             if constexpr (!PLAIN) keep_apart(k);
@@ -381,17 +413,14 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
                 constexpr int QB = S::block(J);
                 const unsigned k_next = k_lane + (J == UNITS - 1 ? sub_base(k + 1, 0) : sub_base(k, 1));
                 const unsigned v_next = v_lane + (S::wrap(J - 2) == UNITS - 1 ? sub_base(k, 0) : sub_base(k, 1));
-                prompt_phase<S, J, true, true, true, !PLAIN || J == 0>(w, c, k_next, v_next, [&](auto i_) __attribute__((always_inline)) {
+                constexpr bool RAW = CAP && (J == 0 ? RAW_BEFORE : PLAIN);
+                prompt_phase<S, J, true, true, true, !PLAIN || J == 0, RAW>(w, RAW ? raw : done, k_next, v_next, [&](auto i_) __attribute__((always_inline)) {
                     GRAFT_CONST(i, i_);
                     constexpr int at = S::SLOTS * J + i, SPACE = S::SLOTS * UNITS / S::LOADS / 2;
                     if constexpr (at == 0) next = page_of(k + 3);
                     if constexpr (at > 0 && at % SPACE == 0 && at / SPACE <= S::LOADS) move(next, at / SPACE - 1);
                 });
-                if constexpr (CAP) {
-                    settle_scores(w.s[QB]);
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) w.s[QB][x] = capped(w.s[QB][x], p.cap_in, p.cap_log2e);
-                }
+                if constexpr (CAP && !PLAIN) cap_scores(w.s[QB]);
                 if constexpr (!PLAIN) hide<S, QB>(w, (st0 + k) * PA_STAGE + (J / NB) * PA_SUB, half, p.window);
             });
         };
@@ -418,17 +447,22 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_attn_kernel(const int32_
             for (int k = 0; k < n_st;) {         // (loops of their own: the registers stay where they are from stage to stage)
                 const int masked_to = k < plain_from ? (plain_from < n_st ? plain_from : n_st) : (k < plain_to ? k : n_st);
                 while (k < masked_to) {
-                    stage(k, std::false_type{});
+                    stage(k, std::false_type{}, std::false_type{});
+                    next_pages(++k);
+                }
+                if (CAP && k < plain_to) {
+                    stage(k, std::true_type{}, std::false_type{});
                     next_pages(++k);
                 }
                 while (k < plain_to) {
-                    stage(k, std::true_type{});
+                    stage(k, std::true_type{}, std::bool_constant<CAP>{});
                     next_pages(++k);
                 }
+                if (CAP && k > plain_from && k == plain_to) cap_scores(w.s[S::block(UNITS - 1)]);
             }
             const auto nothing = [](auto) {};
-            prompt_phase<S, 0, false, true, true, true>(w, c, 0u, 0u, nothing);
-            prompt_phase<S, 1, false, false, true, false>(w, c, 0u, 0u, nothing);
+            prompt_phase<S, 0, false, true, true, true, false>(w, done, 0u, 0u, nothing);
+            prompt_phase<S, 1, false, false, true, false, false>(w, done, 0u, 0u, nothing);
             GRAFT_MFMA_SETTLE();
             GRAFT_WAIT_VMCNT(0);                 // (transfers of stages that are not there)
             lds_barrier();

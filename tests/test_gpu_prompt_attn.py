@@ -28,6 +28,9 @@ CASES = [
     ("bf16", 1, 400, 2, 2, 128, 100, None, "head", 128, 0.0),
     ("bf16", 1, 100, 4, 2, 128, 333, None, "head", 0, 20.0),
     ("bf16", 2, 100, 4, 2, 64, [333, 64], [100, 50], "token", 70, 50.0),
+    ("bf16", 1, 300, 4, 2, 128, 1200, None, "head", 0, 8.0),                # many stages with a cap, behind and in front of partly hidden ones
+    ("bf16", 1, 300, 4, 2, 64, 1200, None, "head", 640, 8.0),
+    ("bf16", 1, 260, 2, 2, 128, 700, None, "head", 449, 100.0),
     ("f32", 2, 130, 6, 2, 128, [0, 77], [130, 60], "token", 0, 0.0),
     ("f32", 1, 200, 4, 1, 64, 500, None, "gap", 0, 0.0),
     ("f32", 1, 100, 4, 4, 128, 200, None, "head", 33, 0.0),
