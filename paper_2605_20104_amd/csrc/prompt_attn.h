@@ -68,10 +68,24 @@ __device__ __forceinline__ float capped(float x, float cap_in, float cap_log2e) 
     const float e = __builtin_amdgcn_exp2f(x * cap_in);
     return __builtin_fmaf(-2.f * cap_log2e, __builtin_amdgcn_rcpf(1.f + e), cap_log2e);
 }
+// The same for fp32 attention: small arguments, where the difference above keeps few bits, by tanh's odd polynomial (up to |z| = 0.45
+// the terms to z^13 of its series are within 2^-25 of it; the argument is 2 z log2(e)).
+__device__ __forceinline__ float capped_f32(float x, float cap_in, float cap_log2e) {
+    const float u = x * cap_in, z = u * 0.34657359028f, w = z * z;
+    float s = __builtin_fmaf(w, 21844.f / 6081075.f, -1382.f / 155925.f);
+    s = __builtin_fmaf(w, s, 62.f / 2835.f);
+    s = __builtin_fmaf(w, s, -17.f / 315.f);
+    s = __builtin_fmaf(w, s, 2.f / 15.f);
+    s = __builtin_fmaf(w, s, -1.f / 3.f);
+    s = __builtin_fmaf(w * z, s, z);
+    const float far = __builtin_fmaf(-2.f * cap_log2e, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u)), cap_log2e);
+    return __builtin_fabsf(z) < 0.45f ? s * cap_log2e : far;
+}
 
-constexpr int PA_BF16_ROWS = 256, PA_F32_ROWS = 128;               // rows of a tile
+constexpr int PA_BF16_ROWS = 256, PA_F32_ROWS = 128, PA_FEW_ROWS = 32;             // rows of a tile
 int32_t launch_prompt_f32(const PromptParams& p, int32_t D, bool cap, hipStream_t s);
 int32_t launch_prompt_bf16(const PromptParams& p, int32_t D, bool cap, hipStream_t s);
+int32_t launch_prompt_few_f32(const PromptParams& p, int32_t D, bool cap, hipStream_t s);
 int32_t launch_prompt_few(const PromptParams& p, int32_t D, bool cap, int32_t tile_rows, hipStream_t s);     // tiles of 32 or 64 rows, bf16
 
 }  // namespace graft

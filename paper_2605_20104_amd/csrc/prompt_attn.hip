@@ -7,70 +7,109 @@ namespace graft {
 
 // Few row tiles leave compute units without work: their keys are cut into splits, whose unnormalised rows go through memory in fp32
 // and are joined by their references and sums.
+// A wavefront a row: lane s has split s's reference and sum, then every lane its D / 64 elements of all splits' rows, eight in flight.
+static_assert(PA_MAX_SPLITS <= 64, "a lane each");
+template <int DPP_CTRL> __device__ __forceinline__ float add_dpp(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), DPP_CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum_f32(float v) {
+    v = add_dpp<0xB1>(v);
+    v = add_dpp<0x4E>(v);
+    v = add_dpp<0x141>(v);
+    v = add_dpp<0x140>(v);
+    unsigned u = __float_as_uint(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    u = __float_as_uint(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
 template <int D, class T>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(const int32_t* n_nodes, const int32_t* prefix_len, PromptParams p) {
-    constexpr int LANES = D / 4, ROWS = 256 / LANES;               // lanes a row, four elements each
-    const int lane = threadIdx.x % LANES, per = (p.R + ROWS - 1) / ROWS, bg = blockIdx.x / per,
-              r = (blockIdx.x - bg * per) * ROWS + threadIdx.x / LANES, b = bg / p.Hkv, g = bg - b * p.Hkv;
+    constexpr int EACH = D / 64, AHEAD = 8;
+    typedef float part_t __attribute__((ext_vector_type(EACH)));
+    const int lane = threadIdx.x & 63, per = (p.R + 3) / 4, bg = blockIdx.x / per;
+    const int r = __builtin_amdgcn_readfirstlane((blockIdx.x - bg * per) * 4 + (threadIdx.x >> 6)), b = bg / p.Hkv, g = bg - b * p.Hkv;
     if (r >= p.R) return;
+    const size_t part = static_cast<size_t>(bg) * p.n_splits * p.R + r;
+    const float* from = p.ws_o + part * D + EACH * lane;
+    const size_t step = static_cast<size_t>(p.R) * D;
+    const float2 ml = lane < p.n_splits ? reinterpret_cast<const float2*>(p.ws_ml)[part + static_cast<size_t>(lane) * p.R] : float2{0.f, 0.f};
+    part_t o[AHEAD];
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) o[s] = *reinterpret_cast<const part_t*>(from + (s < p.n_splits ? s : 0) * step);
     const PromptLengths len = prompt_lengths(p, scalar_load(prefix_len, b), scalar_load(n_nodes, b));
     const int i = div_any(r, p.g_magic, p.g_shift);
-    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
-    if (i < len.n) {
-        const size_t part = static_cast<size_t>(bg) * p.n_splits * p.R + r;
-        const float2* ml = reinterpret_cast<const float2*>(p.ws_ml);
-        float m = -INFINITY;
-        for (int s = 0; s < p.n_splits; ++s) {
-            const float2 x = ml[part + static_cast<size_t>(s) * p.R];
-            m = __builtin_fmaxf(m, x.y != 0.f ? x.x : -INFINITY);   // (a sum of zero: nothing seen; NaN passes)
-        }
-        for (int s = 0; s < p.n_splits; ++s) {
-            const size_t at = part + static_cast<size_t>(s) * p.R;
-            const float2 x = ml[at];
-            const floatx4 o = *reinterpret_cast<const floatx4*>(p.ws_o + at * D + 4 * lane);
-            const float f = x.y != 0.f ? __builtin_amdgcn_exp2f(x.x - m) : 0.f;
-            total += x.y * f;
+    // (a sum of zero: the split saw nothing; NaN passes)
+    const float m = wave_max_f32(lane < p.n_splits && ml.y != 0.f ? ml.x : -INFINITY), f = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
+    const float total = wave_sum_f32(ml.y * f);
+    part_t sum = part_t(0.f);
+    for (int s0 = 0; s0 < p.n_splits; s0 += AHEAD) {
+        if (s0 > 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sum[j] += x.y != 0.f ? o[j] * f : 0.f;
+            for (int s = 0; s < AHEAD; ++s) o[s] = *reinterpret_cast<const part_t*>(from + (s0 + s < p.n_splits ? s0 + s : 0) * step);
         }
-        const float inv = total != 0.f ? 1.f / total : 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] *= inv;
+        for (int s = 0; s < AHEAD; ++s)
+            if (s0 + s < p.n_splits) {
+                const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), s0 + s));
+                if (w != 0.f) sum += o[s] * w;   // (uniform)
+            }
     }
-    const size_t to = ((static_cast<size_t>(b) * p.T + i) * p.Hq + g * p.G + (r - i * p.G)) * D + 4 * lane;
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<uintx2*>(static_cast<unsigned short*>(p.out) + to) = uintx2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
-    else *reinterpret_cast<floatx4*>(static_cast<float*>(p.out) + to) = sum;
+    const float inv = total != 0.f ? 1.f / total : 0.f;
+    if (i < len.n) sum *= inv;
+    else sum = part_t(0.f);
+    const size_t to = ((static_cast<size_t>(b) * p.T + i) * p.Hq + g * p.G + (r - i * p.G)) * D + EACH * lane;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<part_t*>(static_cast<float*>(p.out) + to) = sum;
+    else if constexpr (EACH == 2) *reinterpret_cast<unsigned*>(static_cast<unsigned short*>(p.out) + to) = pack_bf16(sum[0], sum[1]);
+    else static_cast<unsigned short*>(p.out)[to] = static_cast<unsigned short>(pack_bf16(sum[0], 0.f));
 }
 
+// A kernel and its splits, by an estimate of what a launch takes: rounds of the compute units (`per_cu` workgroups each) times a tile's
+// share of the keys, stage by stage, and its set-up; a stage takes what the matrix cores take, or memory for all that run at once; splits
+// add a launch and the partial rows' way through memory.  The host knows the table's capacity, not the lengths: where there are several
+// sequences, half of the estimate is for ones that fill it, half for ragged ones, three quarters of it in the mean, whose workgroups end one by one.
+// Measured with the splits given (us, 32 heads on 8, D = 128; rows of a tile, splits): 1 token behind 2000: 32 rows, 1: 21, 4: 14.0, 8:
+// 12.1, 16: 12.5; behind 65536: 8: 67, 16: 48.1, 32: 51.1; 32 ragged sequences' tokens behind 16384: 1: 305, 4: 278, 8: 282; 32 tokens behind
+// 32768: 64 rows, 16: 43.6, 256 rows, 32: 50.8; 64 behind 2048: 64 rows, 6: 20.7, 256 rows, 8: 29.6; 48 behind 32768: 64 rows, 8: 65.6, 256 rows,
+// 32: 55.4; 256 behind 2048: 1: 65, 6: 37.7, 12: 56.7; 1024 behind 32768, 40 heads: 1: 719, 3: 621, 4: 679.
+struct PromptKernel { int32_t rows, stage, per_cu; double stage_us, setup_us; };      // rows of a tile, keys of a stage
 struct PromptPlan { int32_t tile_rows, n_row_tiles, n_splits; size_t o_bytes, bytes; };
-#ifndef PA_FEW
-#define PA_FEW 64
-#endif
-// A kernel and its splits, by what a launch takes: rounds of the compute units times a tile's share of the keys and its set-up, and for splits
-// a launch and the partial rows' way through memory.  The host knows the table's capacity, not the lengths: half of the cost is
-// that of sequences that fill it, half that of ragged ones, three quarters of it in the mean, whose workgroups end one by one.
 static PromptPlan prompt_plan(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_pages, int32_t dtype, int32_t window) {
-    const bool f32 = dtype == GRAFT_F32;
+    const bool f32 = dtype == GRAFT_F32, wide = D == 128;
     const int32_t G = Hq / Hkv;
     const int64_t R = static_cast<int64_t>(T) * G, units = static_cast<int64_t>(B) * Hkv, cus = device_compute_units();
-    struct Kernel { int32_t rows, stage, per_cu; double stage_us, setup_us; };
-    const Kernel kernel = f32 ? Kernel{PA_F32_ROWS, 32, 2, D == 128 ? 8.0 : 4.0, 3.0}
-                        : R <= 32 ? Kernel{32, 128, 1, D == 128 ? 2.7 : 1.4, 4.0}
-                        : R <= PA_FEW ? Kernel{64, 128, 1, D == 128 ? 2.7 : 1.5, 4.0} : Kernel{PA_BF16_ROWS, 64, D == 128 ? 1 : 2, D == 128 ? 1.2 : 1.4, 4.0};
-    const int64_t tiles = (R + kernel.rows - 1) / kernel.rows, places = cus * kernel.per_cu;
-    int64_t keys = static_cast<int64_t>(max_pages) * GRAFT_PAGE_SIZE;
-    const int64_t reach = static_cast<int64_t>(window) + kernel.rows / G + 1;
-    if (window > 0 && reach < keys) keys = reach;
-    const int64_t stages = (keys + kernel.stage - 1) / kernel.stage;
-    PromptPlan best{kernel.rows, static_cast<int32_t>(tiles), 1, 0, 0};
-    double cost = -1.0;
-    for (int64_t s = 1; s <= PA_MAX_SPLITS && s <= stages && tiles * units * s < (1 << 23); ++s) {
-        const double jobs = static_cast<double>(tiles * units * s), per = static_cast<double>((stages + s - 1) / s) * kernel.stage_us + kernel.setup_us;
-        const double even = std::ceil(jobs / places) * per, last = 0.75 * jobs / places * per + 0.5 * per, ragged = last > per ? last : per;
-        double now = 0.5 * (even + ragged);
-        if (s > 1) now += 4.0 + static_cast<double>(R * units * s) * D * 4 * 2 / 4e6;
-        if (cost < 0 || now < cost) { cost = now; best.n_splits = static_cast<int32_t>(s); }
+    const PromptKernel bf16_kernels[] = {{PA_FEW_ROWS, 128, 1, wide ? 1.3 : 0.8, 5.0}, {2 * PA_FEW_ROWS, 128, 1, wide ? 2.0 : 1.2, 5.0},
+                                         {PA_BF16_ROWS, 64, wide ? 1 : 2, wide ? 1.8 : 2.0, 5.0}};
+    const PromptKernel f32_kernels[] = {{PA_FEW_ROWS, 128, 1, wide ? 5.0 : 2.5, 5.0}, {PA_F32_ROWS, 32, 2, wide ? 7.6 : 3.8, 5.0}};
+    PromptPlan best{0, 0, 0, 0, 0};
+    double cost = 0.0;
+    auto look = [&](const PromptKernel& kernel) {
+        const int64_t tiles = (R + kernel.rows - 1) / kernel.rows, places = cus * kernel.per_cu;
+        int64_t keys = static_cast<int64_t>(max_pages) * GRAFT_PAGE_SIZE;
+        const int64_t reach = static_cast<int64_t>(window) + kernel.rows / G + 1;
+        if (window > 0 && reach < keys) keys = reach;
+        const int64_t stages = (keys + kernel.stage - 1) / kernel.stage;
+        const double stage_bytes = 2.0 * kernel.stage * D * (f32 ? 4 : 2);
+        for (int64_t s = 1; s <= PA_MAX_SPLITS && s <= stages && tiles * units * s < (1 << 23); ++s) {
+            const double jobs = static_cast<double>(tiles * units * s), at_once = jobs < places ? jobs : places;
+            const double memory_us = at_once / tiles * stage_bytes / 5.6e6;       // (the tiles of a unit share what they read)
+            const double per = static_cast<double>((stages + s - 1) / s) * (memory_us > kernel.stage_us ? memory_us : kernel.stage_us) + kernel.setup_us;
+            const double even = std::ceil(jobs / places) * per, last = 0.75 * jobs / places * per + 0.5 * per, ragged = last > per ? last : per;
+            double now = B > 1 ? 0.5 * (even + ragged) : even;
+            if (s > 1) now += 3.0 + static_cast<double>(R * units * s) * D * 4 * 2 / 4e6;
+            if (best.n_splits == 0 || now < cost) {
+                cost = now;
+                best = {kernel.rows, static_cast<int32_t>(tiles), static_cast<int32_t>(s), 0, 0};
+            }
+        }
+    };
+    if (f32) {
+        if (R <= PA_FEW_ROWS) look(f32_kernels[0]);
+        else look(f32_kernels[1]);
+    } else if (R <= PA_FEW_ROWS) look(bf16_kernels[0]);
+    else {
+        if (R <= 2 * PA_BF16_ROWS) look(bf16_kernels[1]);
+        look(bf16_kernels[2]);
     }
     if (best.n_splits > 1) {
         const size_t rows = static_cast<size_t>(R) * units * best.n_splits;
@@ -123,12 +162,13 @@ extern "C" int32_t graft_prompt_attn(const void* q, const void* k_cache, const v
                          !std::signbit(scale) ? 0u : dtype == GRAFT_F32 ? 0x80000000u : 0x80008000u, std::fabs(in), std::fabs(cap_in), softcap * log2e};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool cap = softcap > 0.f;
-    const int32_t rc = dtype == GRAFT_F32 ? launch_prompt_f32(p, D, cap, s)
+    const int32_t rc = plan.tile_rows == PA_FEW_ROWS && dtype == GRAFT_F32 ? launch_prompt_few_f32(p, D, cap, s)
+                     : dtype == GRAFT_F32 ? launch_prompt_f32(p, D, cap, s)
                      : plan.tile_rows < PA_BF16_ROWS ? launch_prompt_few(p, D, cap, plan.tile_rows, s) : launch_prompt_bf16(p, D, cap, s);
     if (rc != GRAFT_OK || plan.n_splits == 1) return rc;
-    auto merge = [&](auto kernel, int rows) { hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>((p.R + rows - 1) / rows) * B * Hkv), dim3(256), 0, s, n_nodes, prefix_len, p); };
-    if (dtype == GRAFT_F32) { if (D == 128) merge(prompt_merge_kernel<128, float>, 8); else merge(prompt_merge_kernel<64, float>, 16); }
-    else if (D == 128) merge(prompt_merge_kernel<128, unsigned short>, 8);
-    else merge(prompt_merge_kernel<64, unsigned short>, 16);
+    auto merge = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>((p.R + 3) / 4) * B * Hkv), dim3(256), 0, s, n_nodes, prefix_len, p); };
+    if (dtype == GRAFT_F32) { if (D == 128) merge(prompt_merge_kernel<128, float>); else merge(prompt_merge_kernel<64, float>); }
+    else if (D == 128) merge(prompt_merge_kernel<128, unsigned short>);
+    else merge(prompt_merge_kernel<64, unsigned short>);
     return check_launch();
 }

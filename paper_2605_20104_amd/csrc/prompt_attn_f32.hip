@@ -127,7 +127,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void prompt_attn_f32_kernel(const in
             }
             if constexpr (CAP) {
 #pragma unroll
-                for (int x = 0; x < 16; ++x) s[x] = capped(s[x], p.cap_in, p.cap_log2e);
+                for (int x = 0; x < 16; ++x) s[x] = capped_f32(s[x], p.cap_in, p.cap_log2e);
             }
             if (!plain) {
                 const int rel = lim - t0 - 4 * half;
