@@ -581,7 +581,7 @@ int32_t graft_prompt_attn(const void* q, const void* k_cache, const void* v_cach
  * status [B]: GRAFT_STATUS_BAD_LENGTH if ctx_len is outside [0,L_max] or start outside [0,ctx_len]; then nothing is counted (the row is
  * zeros, or with start as it was).  counts overlaps none of the inputs.
  *
- * 1 <= B <= 65535, 1 <= L_max < 2^30, V >= 1.
+ * 1 <= B <= 65535, 1 <= L_max < 2^30, 1 <= V < 2^30.
  */
 int32_t graft_token_counts(const int32_t* ctx, const int32_t* ctx_len, const int32_t* prompt_len, const int32_t* start, int32_t B,
                            int32_t L_max, int32_t V, int32_t* counts, int32_t* status, void* stream);

@@ -370,7 +370,7 @@ static AdjustPlan adjust_plan(int32_t B, int32_t K_max, int32_t V) {
 }  // namespace graft
 
 extern "C" size_t graft_logits_adjust_workspace_bytes(int32_t B, int32_t K_max, int32_t V) {
-    if (B < 1 || K_max < 1 || V < 1) return 0;
+    if (B < 1 || K_max < 1 || V < 1 || V >= (1 << 30)) return 0;
     const int64_t rows = static_cast<int64_t>(B) * K_max;
     const graft::AdjustPlan a = graft::adjust_plan(B, K_max, V);
     return static_cast<size_t>(rows) * a.blocks * (graft::LA_THREADS / 64) * sizeof(graft::u64);

@@ -49,23 +49,25 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_few_f32_kernel(const int
         for (int j = 0; j < 2; ++j) x.at[j] = static_cast<int64_t>(scalar_load(table, 2 * s + j < top ? 2 * s + j : top)) * p.page_stride + g * p.head_stride;
         return x;
     };
-    // (tokens behind the last are the last one again: not seen, and values zeros)
     floatx4 key[DC];
-    auto load_keys = [&](int s, const Pages& pg) __attribute__((always_inline)) {
+    auto load_keys = [&](int s, const Pages& pg) __attribute__((always_inline)) {      // (tokens behind the last: the last one, which is not seen there)
         const int left = last_tok - s * PV_STEP, at = l32 < left ? l32 : left;
         const float* k = static_cast<const float*>(p.k) + (at >= 16 ? pg.at[1] : pg.at[0]) + (at & 15) * p.token_stride + 4 * half;
 #pragma unroll
         for (int c = 0; c < DC; ++c) key[c] = *reinterpret_cast<const floatx4*>(k + 8 * c);
     };
+    // Values through descriptors that end with the sequence's last token: zeros behind it, and one address register for all rows.
     float val[16][DE];
+    const unsigned ts4 = static_cast<unsigned>(p.token_stride) * 4u, v_lane = 4u * half * ts4 + 4u * l32;
     auto load_values = [&](int s, const Pages& pg) __attribute__((always_inline)) {
-        const int left = last_tok - s * PV_STEP;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const int want = 8 * (j >> 2) + 4 * half + (j & 3), at = want < left ? want : left;
-            const float* v = static_cast<const float*>(p.v) + (at >= 16 ? pg.at[1] : pg.at[0]) + (at & 15) * p.token_stride + l32;
+            const int rows = last_tok - s * PV_STEP - 16 * (j >> 3);
+            const unsigned bytes = rows >= 0 ? static_cast<unsigned>(rows < 15 ? rows : 15) * ts4 + 4 * D : 0u;
+            const auto from = merge_buffer(static_cast<const float*>(p.v) + pg.at[j >> 3], bytes);
 #pragma unroll
-            for (int e = 0; e < DE; ++e) val[j][e] = v[32 * e];
+            for (int e = 0; e < DE; ++e)
+                val[j][e] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, static_cast<int>(v_lane + 128u * e), static_cast<int>((8u * ((j >> 2) & 1) + (j & 3)) * ts4), 0));
         }
     };
     floatx4 q[DC];
@@ -94,21 +96,13 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_few_f32_kernel(const int
             for (int d = 0; d < DC; ++d)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x = __builtin_amdgcn_mfma_f32_32x32x2f32(key[d][j], q[d][j], x, 0, 0, 0);
-            if (s + AT_WAVES < st1) {
-                pg = pages_of(s + AT_WAVES);
-                load_keys(s + AT_WAVES, pg);
-            }
             __builtin_amdgcn_sched_barrier(0);
             if (!plain) {
                 bool odd = false;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const bool there = t0 + 8 * (j >> 2) + 4 * half + (j & 3) <= last_tok;
 #pragma unroll
-                    for (int e = 0; e < DE; ++e) {
-                        val[j][e] = there ? val[j][e] : 0.f;
-                        odd |= pv_no_number(val[j][e]);
-                    }
+                    for (int e = 0; e < DE; ++e) odd |= pv_no_number(val[j][e]);
                 }
                 if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
                     // values that are not numbers: added to the rows that see them, zeros from here on (0 times them would reach the others)
@@ -165,6 +159,12 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_few_f32_kernel(const int
                 x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], c, negm));
                 l += x[j];
             }
+            __builtin_amdgcn_sched_barrier(0);
+            if (s + AT_WAVES < st1) {
+                pg = pages_of(s + AT_WAVES);
+                load_keys(s + AT_WAVES, pg);
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < 16; ++j)
 #pragma unroll

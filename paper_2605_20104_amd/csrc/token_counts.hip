@@ -8,6 +8,7 @@
 namespace graft {
 
 constexpr int TC_THREADS = 512;
+constexpr int TC_AHEAD = 8;                      // 16-byte loads of the context in flight per thread
 constexpr int TC_SLICE = 8192;                   // counters of a workgroup, 32 KB of LDS
 constexpr int32_t TC_PROMPT = INT32_MIN;         // the bit of tokens that the prompt holds
 typedef int32_t int4u __attribute__((ext_vector_type(4), aligned(4)));
@@ -21,13 +22,13 @@ __device__ __forceinline__ ContextRange context_range(const int32_t* len, const 
 __global__ __launch_bounds__(TC_THREADS) void token_counts_kernel(const int32_t* __restrict__ ctx, const int32_t* __restrict__ ctx_len,
                                                                   const int32_t* __restrict__ prompt_len, int32_t L_max, int32_t V, int32_t per,
                                                                   int32_t* __restrict__ counts, int32_t* __restrict__ status) {
-    __shared__ int32_t n_of[TC_SLICE];
+    __shared__ __attribute__((aligned(16))) int32_t n_of[TC_SLICE];
     const int b = blockIdx.y, tid = threadIdx.x;
     const ContextRange r = context_range(ctx_len, nullptr, b, L_max);
     const int32_t prompt = prompt_len ? prompt_len[b] : 0, to = r.ok ? r.to : 0;
-    const int32_t v0 = blockIdx.x * per, size = V - v0 < per ? V - v0 : per;
+    const int32_t v0 = blockIdx.x * per, rest = V - v0, size = rest < 0 ? 0 : rest < per ? rest : per;
     const int32_t* row = ctx + static_cast<size_t>(b) * L_max;
-    for (int32_t v = tid; v < size; v += TC_THREADS) n_of[v] = 0;
+    for (int32_t v = 4 * tid; v < size; v += 4 * TC_THREADS) *reinterpret_cast<int4*>(n_of + v) = int4{0, 0, 0, 0};
     __syncthreads();
     auto take = [&](int32_t tok, int32_t t) __attribute__((always_inline)) {
         const uint32_t at = static_cast<uint32_t>(tok) - static_cast<uint32_t>(v0);
@@ -36,15 +37,27 @@ __global__ __launch_bounds__(TC_THREADS) void token_counts_kernel(const int32_t*
         else atomicAdd(&n_of[at], 1);
     };
     const int32_t quads = to / 4;
-    for (int32_t q = tid; q < quads; q += TC_THREADS) {
-        const int4u x = *reinterpret_cast<const int4u*>(row + 4 * static_cast<size_t>(q));
+    for (int32_t q0 = tid; q0 < quads; q0 += TC_AHEAD * TC_THREADS) {
+        int4u x[TC_AHEAD];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) take(x[k], 4 * q + k);
+        for (int u = 0; u < TC_AHEAD; ++u) {
+            const int32_t q = q0 + u * TC_THREADS;
+            x[u] = q < quads ? *reinterpret_cast<const int4u*>(row + 4 * static_cast<size_t>(q)) : int4u{-1, -1, -1, -1};
+        }
+#pragma unroll
+        for (int u = 0; u < TC_AHEAD; ++u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) take(x[u][k], 4 * (q0 + u * TC_THREADS) + k);
     }
     if (tid < to - 4 * quads) take(row[4 * quads + tid], 4 * quads + tid);
     __syncthreads();
     int32_t* out = counts + static_cast<size_t>(b) * V + v0;
-    for (int32_t v = tid; v < size; v += TC_THREADS) out[v] = n_of[v];
+    const int32_t full = size & ~3;
+    for (int32_t v = 4 * tid; v < full; v += 4 * TC_THREADS) {
+        const int4 x = *reinterpret_cast<const int4*>(n_of + v);
+        *reinterpret_cast<int4u*>(out + v) = int4u{x.x, x.y, x.z, x.w};
+    }
+    if (tid < size - full) out[full + tid] = n_of[full + tid];
     if (blockIdx.x == 0 && tid == 0) status[b] = r.ok ? 0 : GRAFT_STATUS_BAD_LENGTH;
 }
 
@@ -73,14 +86,14 @@ extern "C" int32_t graft_token_counts(const int32_t* ctx, const int32_t* ctx_len
                                       int32_t L_max, int32_t V, int32_t* counts, int32_t* status, void* stream) {
     using namespace graft;
     if (!ctx || !ctx_len || !counts || !status) return GRAFT_ERR_NULL;
-    if (B < 1 || B > 65535 || L_max < 1 || L_max >= (1 << 30) || V < 1) return GRAFT_ERR_SHAPE;
+    if (B < 1 || B > 65535 || L_max < 1 || L_max >= (1 << 30) || V < 1 || V >= (1 << 30)) return GRAFT_ERR_SHAPE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (start) {
         const int32_t groups = (L_max + TC_THREADS - 1) / TC_THREADS;
         hipLaunchKernelGGL(token_counts_add_kernel, dim3(groups < 16 ? groups : 16, B), dim3(TC_THREADS), 0, s, ctx, ctx_len, prompt_len, start, L_max, V,
                            counts, status);
     } else {
-        const int32_t slices = (V - 1) / TC_SLICE + 1, per = (V - 1) / slices + 1;
+        const int32_t slices = (V - 1) / TC_SLICE + 1, per = ((V - 1) / slices + 4) & ~3;          // (whole groups of four; the last slice is smaller)
         hipLaunchKernelGGL(token_counts_kernel, dim3(slices, B), dim3(TC_THREADS), 0, s, ctx, ctx_len, prompt_len, L_max, V, per, counts, status);
     }
     return check_launch();

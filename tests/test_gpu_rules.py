@@ -160,3 +160,94 @@ def test_padding_bad_trees_and_bad_states():
     c["tokens"][3, 1] = 1000
     _check(c, "apart")
     assert list(adjusted(**c)[2]) == [1, 2, 2, 0]
+
+
+def _gpu(c):
+    return {k: up(v.view(np.int64) if k == "mask" else v) for k, v in c.items()}
+
+
+def test_odd_parameters():
+    """Repetitions that a quotient by reciprocal does not take, zero, negative, no numbers; frequencies that are no numbers."""
+    for r in (0.0, -2.0, 1e-30, 1e30, np.inf, np.nan, 1.0):
+        c = _case(41, 2, 5, 3001, bias=1)
+        c["repetition"][:] = r
+        _check(c, "apart")
+    for f in (np.inf, np.nan, 1e38):
+        c = _case(42, 2, 5, 3001)
+        c["frequency"][0], c["presence"][1] = f, f
+        _check(c, "apart")
+
+
+def test_counts_that_fill_their_bits():
+    c = _case(43, 1, 4, 1000)
+    c["counts"][0, :4] = [2 ** 31 - 1, -1, PROMPT, 2 ** 24 + 1]
+    c["tokens"][0, 1:] = [0, 1, 5]
+    c["counts"][0, 0] = 2 ** 31 - 2                        # one more on the path fits
+    _check(c, "apart")
+
+
+def test_rows_of_any_address():
+    """Logits, results, counts and biases that start 4 bytes past a 16-byte boundary."""
+    c = _case(44, 2, 3, 1003, bias=2, states=3)
+    want, ids, st = adjusted(**c)
+    gpu = _gpu(c)
+    for x in ("logits", "counts", "bias", "allow"):
+        base = torch.empty(gpu[x].numel() + 1, dtype=gpu[x].dtype, device="cuda")
+        base[1:] = gpu[x].flatten()
+        gpu[x] = base[1:].view(gpu[x].shape)
+    result = torch.empty(want.size + 3, device="cuda")[3:].view(want.shape)
+    result.copy_(gpu["logits"])
+    got = graft.graft_logits_adjust(**gpu, result=result)
+    assert same(result.cpu().numpy(), want) and (got["target_ids"].cpu().numpy() == ids).all()
+
+
+def test_streams_repeats_and_graphs():
+    """Two streams at once, and a graph's replays with eager calls in between: the bits of a single call."""
+    cases = [_case(s, 2, 20, 20011, bias=1, states=4) for s in (45, 46)]
+    wants, gpus = [adjusted(**c) for c in cases], [_gpu(c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    results = [[torch.empty_like(g["logits"]) for _ in range(10)] for g in gpus]
+    outs = [[None] * 10 for _ in range(2)]
+    torch.cuda.synchronize()
+    for rep in range(10):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                outs[i][rep] = graft.graft_logits_adjust(**gpus[i], result=results[i][rep], stream=streams[i])
+    torch.cuda.synchronize()
+    live = lambda x, c: np.concatenate([x[b, :n].ravel() for b, n in enumerate(c["n_nodes"])])              # noqa: E731
+    for i in range(2):
+        for rep in range(10):
+            assert same(live(results[i][rep].cpu().numpy(), cases[i]), live(wants[i][0], cases[i]))
+            assert (outs[i][rep]["target_ids"].cpu().numpy() == wants[i][1]).all()
+    gpu, (B, K, V) = gpus[0], gpus[0]["logits"].shape
+    out = {"target_ids": torch.zeros((B, K), dtype=torch.int32, device="cuda"), "status": torch.zeros(B, dtype=torch.int32, device="cuda")}
+    ws = torch.empty(graft.graft_logits_adjust_workspace_bytes(B, K, V), dtype=torch.uint8, device="cuda")
+    ctx, n, counts = up(np.arange(300, dtype=np.int32).reshape(2, 150)), up(np.array([150, 20], np.int32)), gpu["counts"]
+
+    def step():
+        graft.graft_token_counts(ctx, n, n, counts, status=out["status"])
+        graft.graft_token_counts(ctx, n, None, counts, start=up0, status=out["status"])
+        graft.graft_logits_adjust(**gpu, result=results[0][0], out=out, workspace=ws)
+    up0 = up(np.zeros(2, np.int32))
+    step()
+    torch.cuda.synchronize()
+    eager = [results[0][0].clone(), out["target_ids"].clone(), counts.clone()]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=streams[0]):
+        step()
+    for _ in range(4):
+        results[0][0].zero_()
+        out["target_ids"].zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(results[0][0], eager[0]) and torch.equal(out["target_ids"], eager[1]) and torch.equal(counts, eager[2])
+        step()
+        torch.cuda.synchronize()
+
+
+def test_many_rows():
+    """Several rows a workgroup, in the last of them fewer; trees of every length."""
+    c = _case(47, 8, 48, 9001, n=[48, 47, 33, 1, 8, 9, 17, 16], bias=1, states=5)
+    _check(c, "apart")
+    _check(c, "none")
