@@ -2,7 +2,7 @@
 //
 // One pass over the logits.  Counts and biases belong to a sequence, not to a node: a workgroup takes a block of the vocabulary's columns
 // for several of a sequence's rows, makes of counts and biases what every row needs of them (which tokens have been seen, what to
-// subtract, what to add) and keeps that in registers while the rows pass, the next one's logits on their way.  What a node's path adds
+// subtract, what to add) and keeps that in LDS, each thread its own columns, while the rows pass, the next one's logits on their way.  What a node's path adds
 // to its history is a handful of tokens, found by comparing and done over for the threads that have them.  Columns are the same for
 // all rows, whatever a row's address: loads of 16 bytes need not be aligned.
 //
@@ -14,9 +14,9 @@ namespace graft {
 
 constexpr int LA_THREADS = 256, LA_QUADS = 2;    // 2048 columns a block
 // Rows of a workgroup: as many as leave LA_FILL workgroups, up to LA_ROWS.  Its columns' set-up (a trip to memory, two barriers) is worth
-// several rows: us a call, everything on, 8 x 48 rows of 151936 written / 3 x 31 of 50257: 1 row 127 / 18 (counts and biases read by every
-// row), 4 rows 99.2 / 13.3, 8 rows 94.5 / 12.3, 16 rows 96 to 98 / 12.3; LA_FILL 2048 94.5 / 13.0, 512 97.8 / 15.1.  With groups of
-// four columns by one and four a thread 104 / 13.5 and 102 / 15.7.
+// several rows: us a call in a graph, everything on, 8 x 48 rows of 151936 written / 3 x 31 of 50257, ids only: 1 row 127 / 15.0 (counts and biases read by every
+// row), 4 rows 99.2 / 13.3, 8 rows 94.5 / 12.3, 16 rows 96 to 98 / 12.3; LA_FILL 2048 13.0 for the second, 512 97.8 / 15.1.  With groups of
+// four columns by one and four a thread 104 / 14.0 and 102 to 113 / 15.3.
 constexpr int LA_ROWS = 8;
 constexpr int64_t LA_FILL = 1024;
 typedef int32_t int4u __attribute__((ext_vector_type(4), aligned(4)));      // groups of four columns

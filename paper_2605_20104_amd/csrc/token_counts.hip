@@ -3,6 +3,8 @@
 // Whole rows are counted in LDS: a workgroup has a slice of a sequence's vocabulary, reads the whole context and counts what
 // falls into its slice, so that a row needs no clearing pass, no atomics in memory and one launch.  Additions to rows that
 // are there (a round's few tokens) are atomics in memory: sums and ORs of whole numbers, whose order does not show.
+// Bound by two trips to memory and, for long contexts, by the pass over them: 16 contexts of up to 16K, 151936 tokens, 6.4 us in a graph, one context
+// of a small vocabulary 3.5.  Slices of 4096: 6.9 and 3.4, of 16384 with 1024 threads 6.2 and 3.9 (a context of 300, 32 sequences: 7.1, 6.8 against 6.3).
 #include "common.h"
 
 namespace graft {
