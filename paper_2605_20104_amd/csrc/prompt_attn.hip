@@ -93,6 +93,7 @@ static PromptPlan prompt_plan(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int
         const int64_t stages = (keys + kernel.stage - 1) / kernel.stage;
         const double stage_bytes = 2.0 * kernel.stage * D * (f32 ? 4 : 2);
         for (int64_t s = 1; s <= PA_MAX_SPLITS && s <= stages && tiles * units * s < (1 << 23); ++s) {
+            if (s > 1 && R * units >= (1 << 24)) break;                           // (a merge has 64 lanes a row, a launch's dimension less than 2^32)
             const double jobs = static_cast<double>(tiles * units * s), at_once = jobs < places ? jobs : places;
             const double memory_us = at_once / tiles * stage_bytes / 5.6e6;       // (the tiles of a unit share what they read)
             const double per = static_cast<double>((stages + s - 1) / s) * (memory_us > kernel.stage_us ? memory_us : kernel.stage_us) + kernel.setup_us;

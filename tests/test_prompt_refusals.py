@@ -62,6 +62,14 @@ def test_prompt_attn_workspace_sizes(lib):
     assert w(4, 8192, 32, 8, 128, 512, 0, 1) == 0           # enough tiles for every compute unit
 
 
+# The merge has a wavefront for each row: with rows for 2^32 lanes and more there would be no launch for it, so nothing is split there.
+@pytest.mark.parametrize("B,T,Hq,Hkv,D,dtype", [(1, 2097665, 32, 2, 64, 0), (1, 1048577, 128, 8, 64, 0), (1, 1048577, 32, 2, 64, 0), (3, 1 << 22, 16, 1, 128, 1)])
+def test_prompt_attn_splits_only_what_a_merge_can_take(B, T, Hq, Hkv, D, dtype):
+    rows = B * Hq * T
+    size = graft.graft_prompt_attn_workspace_bytes(B, T, Hq, Hkv, D, 262144, 0, dtype)
+    assert size == 0 or rows * 64 < 1 << 31, size / (rows * (D + 2) * 4)
+
+
 def test_prompt_workspaces_follow_the_current_device(tmp_path):
     (tmp_path / "stand_in.c").write_text(STAND_IN)
     so = str(tmp_path / "stand_in.so")
