@@ -139,7 +139,8 @@ template <class S, int B, bool RAW> __device__ __forceinline__ void raise_refere
             mm = halves_max(mm);
             if (mm + negm > PA_RISE) negm = -mm;
         }
-        const float f = negm < w.negm[b] ? __builtin_amdgcn_exp2f(negm - w.negm[b]) : 1.f;
+        // (a first reference scales nothing: rows have nothing yet, or what keeping apart has added)
+        const float f = negm < w.negm[b] && w.negm[b] != PA_FRESH ? __builtin_amdgcn_exp2f(negm - w.negm[b]) : 1.f;
         w.negm[b] = negm;
         w.late[b] = -INFINITY;
         l *= f;

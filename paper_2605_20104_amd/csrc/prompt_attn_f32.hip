@@ -144,7 +144,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void prompt_attn_f32_kernel(const in
                 float mm = s[0] * c;
 #pragma unroll
                 for (int x = 1; x < 16; ++x) mm = __builtin_fmaxf(mm, s[x] * c);
-                const float now = rise ? -pf_max(mm) : negm, f = rise ? __builtin_amdgcn_exp2f(now - negm) : 1.f;
+                // (a first reference scales nothing: rows have nothing yet, or what keeping apart has added)
+                const float now = rise ? -pf_max(mm) : negm, f = rise && negm != PF_FRESH ? __builtin_amdgcn_exp2f(now - negm) : 1.f;
                 negm = now;
                 l *= f;
 #pragma unroll

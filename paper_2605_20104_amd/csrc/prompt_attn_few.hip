@@ -187,7 +187,8 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_few_kernel(const int32_t
                     float mm = x[0] * c;
 #pragma unroll
                     for (int j = 1; j < 16; ++j) mm = __builtin_fmaxf(mm, x[j] * c);
-                    const float now = rise ? -pw_max(mm) : negm[rb], f = rise ? __builtin_amdgcn_exp2f(now - negm[rb]) : 1.f;
+                    // (a first reference scales nothing: rows have nothing yet, or what keeping apart has added)
+                    const float now = rise ? -pw_max(mm) : negm[rb], f = rise && negm[rb] != PW_FRESH ? __builtin_amdgcn_exp2f(now - negm[rb]) : 1.f;
                     negm[rb] = now;
                     l[rb] *= f;
 #pragma unroll

@@ -148,7 +148,8 @@ __global__ __launch_bounds__(AT_THREADS, 1) void prompt_few_f32_kernel(const int
                 float mm = x[0] * c;
 #pragma unroll
                 for (int j = 1; j < 16; ++j) mm = __builtin_fmaxf(mm, x[j] * c);
-                const float m = rise ? -pv_max(mm) : negm, f = rise ? __builtin_amdgcn_exp2f(m - negm) : 1.f;
+                // (a first reference scales nothing: rows have nothing yet, or what keeping apart has added)
+                const float m = rise ? -pv_max(mm) : negm, f = rise && negm != PV_FRESH ? __builtin_amdgcn_exp2f(m - negm) : 1.f;
                 negm = m;
                 l *= f;
 #pragma unroll

@@ -93,3 +93,23 @@ def test_infinities_in_hidden_places(dtype, T, window, bad):
             elif which == "v":
                 assert not torch.isfinite(row[:, 5]).any()
                 assert torch.isfinite(torch.cat([row[:, :5], row[:, 6:]], 1)).all()
+
+
+# What a token does see of infinite values, in the stage of its row's first scores as elsewhere: a positive share of an infinity.
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("P,T,window", [(0, 1, 0), (0, 3, 0), (0, 20, 0), (0, 300, 0), (150, 3, 0), (150, 3, 40), (150, 200, 70), (3000, 2, 0), (3000, 100, 0)])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_infinities_in_seen_places(dtype, P, T, window, bad):
+    c = make(11, dtype, 1, T, 6, 2, 128, P, T)
+    clean = call(c, window).float().cpu()
+    at = sorted({0, P, P + T // 2})
+    d = dict(c, v=c["v"].clone())
+    for t in at:
+        d["v"][d["table"][0, t // 16], 1, t % 16, 5] = bad
+    got = call(d, window).float().cpu()
+    for i in range(T):
+        if any(t <= P + i and (not window or t > P + i - window) for t in at):
+            row = got[0, i, 3:, 5]
+            assert bool((torch.isnan(row) if bad != bad else row == bad).all()), (i, row)
+            got[0, i, 3:, 5] = clean[0, i, 3:, 5]
+    check(c, got, window)
