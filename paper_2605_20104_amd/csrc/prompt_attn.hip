@@ -44,6 +44,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const int32_t* n_node
     // (a sum of zero: the split saw nothing; NaN passes)
     const float m = wave_max_f32(lane < p.n_splits && ml.y != 0.f ? ml.x : -INFINITY), f = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
     const float total = wave_sum_f32(ml.y * f);
+    const u64 some = __builtin_amdgcn_ballot_w64(ml.y != 0.f);      // (not by f: 0 times an infinity is not 0)
     part_t sum = part_t(0.f);
     for (int s0 = 0; s0 < p.n_splits; s0 += AHEAD) {
         if (s0 > 0) {
@@ -54,7 +55,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const int32_t* n_node
         for (int s = 0; s < AHEAD; ++s)
             if (s0 + s < p.n_splits) {
                 const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), s0 + s));
-                if (w != 0.f) sum += o[s] * w;   // (uniform)
+                if ((some >> (s0 + s)) & 1) sum += o[s] * w;                      // (uniform)
             }
     }
     const float inv = total != 0.f ? 1.f / total : 0.f;

@@ -113,3 +113,20 @@ def test_infinities_in_seen_places(dtype, P, T, window, bad):
             assert bool((torch.isnan(row) if bad != bad else row == bad).all()), (i, row)
             got[0, i, 3:, 5] = clean[0, i, 3:, 5]
     check(c, got, window)
+
+
+# ... and where its share is below fp32's smallest number, it is 0 times an infinity: no number, whichever split it lies in.
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 20, 100])
+@pytest.mark.parametrize("at", [3, 700, 1900])
+@pytest.mark.parametrize("low", [1, 2000])
+def test_infinities_without_weight(dtype, T, at, low):
+    c = make(12, dtype, 1, T, 6, 2, 128, 3000, T)
+    c["q"] = c["q"].abs()
+    for t in [at] if low == 1 else range(low):                 # one token, or all of the first splits': scores of some -360, the others within 20 of 0
+        c["k"][c["table"][0, t // 16], :, t % 16] = -40.0
+    tok = (c["table"][0, at // 16], slice(None), at % 16)
+    c["v"][tok] = 0.0
+    check(c, call(c))
+    c["v"][tok] = float("inf")
+    assert not bool(torch.isfinite(call(c)).any())
