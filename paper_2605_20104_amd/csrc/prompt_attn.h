@@ -86,7 +86,7 @@ __device__ __forceinline__ float capped_f32(float x, float cap_in, float cap_log
 constexpr int PA_BF16_ROWS = 256, PA_F32_ROWS = 128, PA_FEW_ROWS = 32;             // rows of a tile
 int32_t launch_prompt_f32(const PromptParams& p, int32_t D, bool cap, hipStream_t s);
 int32_t launch_prompt_bf16(const PromptParams& p, int32_t D, bool cap, hipStream_t s);
-int32_t launch_prompt_few_f32(const PromptParams& p, int32_t D, bool cap, hipStream_t s);
+int32_t launch_prompt_few_f32(const PromptParams& p, int32_t D, bool cap, int32_t tile_rows, hipStream_t s);
 int32_t launch_prompt_few(const PromptParams& p, int32_t D, bool cap, int32_t tile_rows, hipStream_t s);     // tiles of 32 or 64 rows, bf16
 
 }  // namespace graft

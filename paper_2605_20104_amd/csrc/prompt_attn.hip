@@ -75,6 +75,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const int32_t* n_node
 // 12.1, 16: 12.5; behind 65536: 8: 67, 16: 48.1, 32: 51.1; 32 ragged sequences' tokens behind 16384: 1: 305, 4: 278, 8: 282; 32 tokens behind
 // 32768: 64 rows, 16: 43.6, 256 rows, 32: 50.8; 64 behind 2048: 64 rows, 6: 20.7, 256 rows, 8: 29.6; 48 behind 32768: 64 rows, 8: 65.6, 256 rows,
 // 32: 55.4; 256 behind 2048: 1: 65, 6: 37.7, 12: 56.7; 1024 behind 32768, 40 heads: 1: 719, 3: 621, 4: 679.
+// fp32, 16 rows: 1 behind 65536: 16: 132, 20: 111, 24: 100, 32: 103; 8 tokens behind 16000: 1: 463, 2: 243, 3: 183, 5: 248, 8: 185.
 struct PromptKernel { int32_t rows, stage, per_cu; double stage_us, setup_us; };      // rows of a tile, keys of a stage
 struct PromptPlan { int32_t tile_rows, n_row_tiles, n_splits; size_t o_bytes, bytes; };
 static PromptPlan prompt_plan(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_pages, int32_t dtype, int32_t window) {
@@ -83,7 +84,8 @@ static PromptPlan prompt_plan(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int
     const int64_t R = static_cast<int64_t>(T) * G, units = static_cast<int64_t>(B) * Hkv, cus = device_compute_units();
     const PromptKernel bf16_kernels[] = {{PA_FEW_ROWS, 128, 1, wide ? 1.3 : 0.8, 5.0}, {2 * PA_FEW_ROWS, 128, 1, wide ? 2.0 : 1.2, 5.0},
                                          {PA_BF16_ROWS, 64, wide ? 1 : 2, wide ? 1.8 : 2.0, 5.0}};
-    const PromptKernel f32_kernels[] = {{PA_FEW_ROWS, 128, 1, wide ? 5.0 : 2.5, 5.0}, {PA_F32_ROWS, 32, 2, wide ? 7.6 : 3.8, 5.0}};
+    const PromptKernel f32_kernels[] = {{PA_FEW_ROWS / 2, 128, 1, wide ? 3.6 : 1.75, 5.0}, {PA_FEW_ROWS, 128, 1, wide ? 5.0 : 2.5, 5.0},
+                                        {PA_F32_ROWS, 32, 2, wide ? 7.6 : 3.8, 5.0}};
     PromptPlan best{0, 0, 0, 0, 0};
     double cost = 0.0;
     auto look = [&](const PromptKernel& kernel) {
@@ -108,8 +110,9 @@ static PromptPlan prompt_plan(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int
         }
     };
     if (f32) {
-        if (R <= PA_FEW_ROWS) look(f32_kernels[0]);
-        else look(f32_kernels[1]);
+        if (R <= PA_FEW_ROWS / 2) look(f32_kernels[0]);
+        else if (R <= PA_FEW_ROWS) look(f32_kernels[1]);
+        else look(f32_kernels[2]);
     } else if (R <= PA_FEW_ROWS) look(bf16_kernels[0]);
     else {
         if (R <= 2 * PA_BF16_ROWS) look(bf16_kernels[1]);
@@ -166,7 +169,7 @@ extern "C" int32_t graft_prompt_attn(const void* q, const void* k_cache, const v
                          !std::signbit(scale) ? 0u : dtype == GRAFT_F32 ? 0x80000000u : 0x80008000u, std::fabs(in), std::fabs(cap_in), softcap * log2e};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool cap = softcap > 0.f;
-    const int32_t rc = plan.tile_rows == PA_FEW_ROWS && dtype == GRAFT_F32 ? launch_prompt_few_f32(p, D, cap, s)
+    const int32_t rc = plan.tile_rows <= PA_FEW_ROWS && dtype == GRAFT_F32 ? launch_prompt_few_f32(p, D, cap, plan.tile_rows, s)
                      : dtype == GRAFT_F32 ? launch_prompt_f32(p, D, cap, s)
                      : plan.tile_rows < PA_BF16_ROWS ? launch_prompt_few(p, D, cap, plan.tile_rows, s) : launch_prompt_bf16(p, D, cap, s);
     if (rc != GRAFT_OK || plan.n_splits == 1) return rc;

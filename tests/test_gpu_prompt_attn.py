@@ -130,3 +130,12 @@ def test_infinities_without_weight(dtype, T, at, low):
     check(c, call(c))
     c["v"][tok] = float("inf")
     assert not bool(torch.isfinite(call(c)).any())
+
+
+# fp32 with few rows: on either side of 16 and 32 of a KV head, on pages that end inside a step.
+@pytest.mark.parametrize("T,Hq,Hkv", [(1, 2, 2), (1, 16, 1), (5, 6, 2), (8, 4, 2), (16, 1, 1), (17, 1, 1), (4, 32, 4), (11, 6, 2), (33, 2, 2)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("P,window,cap,layout", [(0, 0, 0.0, "head"), (50, 0, 0.0, "gap"), (1001, 300, 0.0, "token"), (4000, 0, 30.0, "head"), (700, 13, 5.0, "token")])
+def test_few_rows_in_fp32(T, Hq, Hkv, D, P, window, cap, layout):
+    c = make(T + P, "f32", 2, T, Hq, Hkv, D, [P, P // 3], [T, max(1, T - 2)], layout)
+    check(c, call(c, window, cap), window, cap)
