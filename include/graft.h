@@ -544,6 +544,7 @@ int32_t graft_kv_compact_mx(void* k_cache, void* v_cache, int64_t layer_stride, 
  * position P + i, P = prefix_len[b]; query head h (KV head g = h / (Hq/Hkv)), with x_t = scale * q[b,i,h,:] . k_t[g,:]:
  *     S   = {tokens t : t <= P + i, and with window > 0 only t > P + i - window}
  *     out[b,i,h,:] = sum_{t in S} softmax_t(y_t) v_t[g,:],   y_t = softcap > 0 ? softcap tanh(x_t / softcap) : x_t
+ * The scale may be zero (the mean of the values of S) or negative.
  *
  *     q, out [B,T,Hq,D]   dtype elements, dense; out may be q itself and overlaps nothing else
  *     caches, strides, block_table, prefix_len   as in graft_tree_attn

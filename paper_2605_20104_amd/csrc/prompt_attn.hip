@@ -162,13 +162,15 @@ extern "C" int32_t graft_prompt_attn(const void* q, const void* k_cache, const v
     if (plan.bytes > 0 && (!workspace || workspace_bytes < plan.bytes || (reinterpret_cast<size_t>(workspace) & 15))) return GRAFT_ERR_WORKSPACE;
     const int32_t G = Hq / Hkv;
     const Magic by_g = magic_any(static_cast<uint32_t>(G));
+    // Hidden scores are -inf, which a scale of zero behind them would make NaN.  A cap of 1 without a cap's scale makes the same zeros of what
+    // is seen (and NaN where 0 times the product is none), in front of what hides.  (A product with log2(e) is zero for a scale of zero only.)
+    const bool flat = in == 0.f && softcap == 0.f, cap = softcap > 0.f || flat;
     float* const ws = static_cast<float*>(workspace);
     const PromptParams p{q, k_cache, v_cache, out, block_table, prefix_len, n_nodes, ws, plan.bytes ? ws + plan.o_bytes / sizeof(float) : nullptr, page_stride,
                          token_stride, head_stride, max_pages, B, T, Hq, Hkv, G, T * G, plan.n_splits, plan.n_row_tiles,
                          window > 0 ? window : INT32_MAX, by_g.m, by_g.shift,
-                         !std::signbit(scale) ? 0u : dtype == GRAFT_F32 ? 0x80000000u : 0x80008000u, std::fabs(in), std::fabs(cap_in), softcap * log2e};
+                         !std::signbit(scale) ? 0u : dtype == GRAFT_F32 ? 0x80000000u : 0x80008000u, std::fabs(in), std::fabs(cap_in), (flat ? 1.f : softcap) * log2e};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool cap = softcap > 0.f;
     const int32_t rc = plan.tile_rows <= PA_FEW_ROWS && dtype == GRAFT_F32 ? launch_prompt_few_f32(p, D, cap, plan.tile_rows, s)
                      : dtype == GRAFT_F32 ? launch_prompt_f32(p, D, cap, s)
                      : plan.tile_rows < PA_BF16_ROWS ? launch_prompt_few(p, D, cap, plan.tile_rows, s) : launch_prompt_bf16(p, D, cap, s);
