@@ -556,7 +556,7 @@ int32_t graft_kv_compact_mx(void* k_cache, void* v_cache, int64_t layer_stride, 
  * second product; GRAFT_F32: fp32 throughout.  A capped score is off by up to 2^-20 of the cap.  Values past 2^100 may overflow in sums.
  *
  * workspace: at least graft_prompt_attn_workspace_bytes(...) bytes (0: NULL will do), 16-byte aligned, scratch; calls that may run at
- * the same time need one each.  It depends on the current device, as graft_tree_attn_workspace_bytes does.
+ * the same time need one each.  It depends on the current device, as graft_tree_attn_workspace_bytes does, and is at most 256 MiB.
  *
  * Requires D in {64,128}, Hq % Hkv == 0, Hq/Hkv <= 16, 1 <= T <= 2^22, 1 <= max_pages <= 262144, B <= 65535, B * Hkv <= 2^18,
  * B * Hkv * ceil(T (Hq/Hkv) / 128) < 2^23, strides that are multiples of 8 elements, token_stride and head_stride at least D, token_stride < 2^26,

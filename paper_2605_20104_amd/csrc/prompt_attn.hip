@@ -76,6 +76,12 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const int32_t* n_node
 // 32768: 64 rows, 16: 43.6, 256 rows, 32: 50.8; 64 behind 2048: 64 rows, 6: 20.7, 256 rows, 8: 29.6; 48 behind 32768: 64 rows, 8: 65.6, 256 rows,
 // 32: 55.4; 256 behind 2048: 1: 65, 6: 37.7, 12: 56.7; 1024 behind 32768, 40 heads: 1: 719, 3: 621, 4: 679.
 // fp32, 16 rows: 1 behind 65536: 16: 132, 20: 111, 24: 100, 32: 103; 8 tokens behind 16000: 1: 463, 2: 243, 3: 183, 5: 248, 8: 185.
+// Partial rows may take what the Infinity Cache holds, 256 MiB.  Past that a split gains the end of a last round where the table is full, and
+// costs most where it is not (us, D = 128, without a split / with two, from an empty cache / in a full table): 4500 tokens of 64 heads, 131072 in the
+// table: 353 / 565, 16530 / 15360; 9000 of 32, 65536: 610 / 800, 7950 / 7430.  (So a merge, with 64 lanes a row, always fits a launch.)
+// Within it a table that is wide and empty still costs: 1100 tokens of 32 heads in 7 splits from an empty cache 101 us where the table has 131072
+// tokens, behind 130000 2060.  A table as wide as what a sequence holds is planned for what it holds.
+constexpr int64_t PA_SPLIT_BYTES = 1 << 28;
 struct PromptKernel { int32_t rows, stage, per_cu; double stage_us, setup_us; };      // rows of a tile, keys of a stage
 struct PromptPlan { int32_t tile_rows, n_row_tiles, n_splits; size_t o_bytes, bytes; };
 static PromptPlan prompt_plan(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_pages, int32_t dtype, int32_t window) {
@@ -96,7 +102,7 @@ static PromptPlan prompt_plan(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int
         const int64_t stages = (keys + kernel.stage - 1) / kernel.stage;
         const double stage_bytes = 2.0 * kernel.stage * D * (f32 ? 4 : 2);
         for (int64_t s = 1; s <= PA_MAX_SPLITS && s <= stages && tiles * units * s < (1 << 23); ++s) {
-            if (s > 1 && R * units >= (1 << 24)) break;                           // (a merge has 64 lanes a row, a launch's dimension less than 2^32)
+            if (s > 1 && R * units * s * (D + 2) * 4 > PA_SPLIT_BYTES) break;
             const double jobs = static_cast<double>(tiles * units * s), at_once = jobs < places ? jobs : places;
             const double memory_us = at_once / tiles * stage_bytes / 5.6e6;       // (the tiles of a unit share what they read)
             const double per = static_cast<double>((stages + s - 1) / s) * (memory_us > kernel.stage_us ? memory_us : kernel.stage_us) + kernel.setup_us;
