@@ -552,8 +552,9 @@ int32_t graft_kv_compact_mx(void* k_cache, void* v_cache, int64_t layer_stride, 
  * Rows of padding tokens are zeros, and so are all rows of a sequence whose prefix_len < 0, n_nodes is outside [0,T] or tokens exceed
  * the block table.  T is not bounded by GRAFT_MAX_NODES.  What a token does not see, an infinity or NaN of its keys or
  * values among it, does not reach the token's rows.
- * dtype GRAFT_BF16: fp32 scores, softmax and sums, probabilities (up to 2^8, relative to a reference of the row) rounded to bf16 for the
- * second product; GRAFT_F32: fp32 throughout.  A capped score is off by up to 2^-20 of the cap.  Values past 2^100 may overflow in sums.
+ * dtype GRAFT_BF16: fp32 scores, softmax and sums, probabilities (relative to a reference of the row: up to 2^8, up to 2^24 of the last 64
+ * tokens) rounded to bf16 for the second product; GRAFT_F32: fp32 throughout.  A capped score is off by up to 2^-20 of the cap.  Values past
+ * 2^96 may overflow in sums.
  *
  * workspace: at least graft_prompt_attn_workspace_bytes(...) bytes (0: NULL will do), 16-byte aligned, scratch; calls that may run at
  * the same time need one each.  It depends on the current device, as graft_tree_attn_workspace_bytes does, and is at most 256 MiB.

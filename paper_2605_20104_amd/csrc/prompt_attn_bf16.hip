@@ -8,8 +8,10 @@
 // comes from the LDS transpose read in that order.
 //
 // Softmax: one pass.  A row's scores are taken relative to a reference, its first maximum; the reference moves when a score
-// passes it by 8 (log2 units), so probabilities stay below 2^8 and accumulated rows are rescaled hardly ever.  Scores,
-// references and sums are fp32; probabilities are rounded to bf16 for the second product, results once at the end.
+// passes it by 8 (log2 units), so accumulated rows are rescaled hardly ever.  Inside the sequence it is looked at once a stage: what a
+// stage adds in between has probabilities of up to 2^24 (past that the tile is done again, every unit checked), everything else of up
+// to 2^8.  So sums stay below (2^22 tokens 2^8 + 64 2^24) = 2^31 times the largest value.  Scores, references and sums are fp32;
+// probabilities are rounded to bf16 for the second product, results once at the end.
 //
 // Bound by the energy of its MFMAs and by issue slots: a stage of 64 tokens and 256 rows (D = 128) takes about 3390 cycles, 2056 of them the MFMAs',
 // at some 1.9 GHz.  1024 tokens of 40 heads behind 32768: 698 GFLOP, 621 us with the merge (1.12 PFLOP/s, where a library product of 8192^3 reaches 1.24);
