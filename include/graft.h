@@ -547,11 +547,13 @@ int32_t graft_kv_compact_mx(void* k_cache, void* v_cache, int64_t layer_stride, 
  * The scale may be zero (the mean of the values of S) or negative.
  *
  *     q, out [B,T,Hq,D]   dtype elements, dense; out may be q itself and overlaps nothing else
- *     caches, strides, block_table, prefix_len   as in graft_tree_attn
+ *     caches, strides, block_table, prefix_len   as in graft_tree_attn; table entries below P + n_nodes[b] are pages of the cache, those
+ *                         in front of a window among them
  *     n_nodes [B]         0 <= n_nodes[b] <= T: lengths of a padded batch
- * Rows of padding tokens are zeros, and so are all rows of a sequence whose prefix_len < 0, n_nodes is outside [0,T] or tokens exceed
- * the block table.  T is not bounded by GRAFT_MAX_NODES.  What a token does not see, an infinity or NaN of its keys or
- * values among it, does not reach the token's rows.
+ * Rows of padding tokens are zeros, and so are rows of which every score is -infinity, and all rows of a sequence whose prefix_len < 0,
+ * n_nodes is outside [0,T] or tokens exceed the block table.  T is not bounded by GRAFT_MAX_NODES.  What a token does not see, an
+ * infinity or NaN of its keys or values among it, does not reach the token's rows.  (Their rounding may go by other tokens' queries in bf16: calls
+ * repeat bit for bit, a row computed among others is within its error of the same row.)  Caches of 4 bits have no such call.
  * dtype GRAFT_BF16: fp32 scores, softmax and sums, probabilities (relative to a reference of the row: up to 2^8, up to 2^24 of the last 64
  * tokens) rounded to bf16 for the second product; GRAFT_F32: fp32 throughout.  A capped score is off by up to 2^-20 of the cap.  Values past
  * 2^96 may overflow in sums.
@@ -592,7 +594,7 @@ int32_t graft_token_counts(const int32_t* ctx, const int32_t* ctx_len, const int
  * graft_logits_adjust - a request's rules on the logits of its tree's nodes, between the target model and graft_accept.  Row i < n_nodes[b] of
  * sequence b scores what follows node i; its history is what counts says (the context up to and with the root) and the nodes
  * below the root on its path.  For token v, with c = counts[b,v] (counts == NULL: 0) as graft_token_counts writes it,
- *     gen = (c & 0x7fffffff) + number of nodes j != 0, bit j of mask[b,i] set, with tokens[b,j] == v,   seen = (bit 31 of c) or gen > 0
+ *     gen = (c & 0x7fffffff) + number of nodes 0 < j < n_nodes[b], bit j of mask[b,i] set, with tokens[b,j] == v,   seen = (bit 31 of c) or gen > 0
  *     x = logits[b,i,v];   seen:    x = x > 0 ? x / repetition[b] : x * repetition[b]
  *                          gen > 0: x = x - gen * frequency[b];  x = x - presence[b]
  *     x = x + bias[v] (or bias[b,v]);   bit v of allow's row allow_index[b,i] clear: x = -infinity

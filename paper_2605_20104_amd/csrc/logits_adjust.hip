@@ -14,9 +14,10 @@ namespace graft {
 
 constexpr int LA_THREADS = 256, LA_QUADS = 2;    // 2048 columns a block
 // Rows of a workgroup: as many as leave LA_FILL workgroups, up to LA_ROWS.  Its columns' set-up (a trip to memory, two barriers) is worth
-// several rows: us a call in a graph, everything on, 8 x 48 rows of 151936 written / 3 x 31 of 50257, ids only: 1 row 127 / 15.0 (counts and biases read by every
-// row), 4 rows 99.2 / 13.3, 8 rows 94.5 / 12.3, 16 rows 96 to 98 / 12.3; LA_FILL 2048 13.0 for the second, 512 97.8 / 15.1.  With groups of
-// four columns by one and four a thread 104 / 14.0 and 102 to 113 / 15.3.
+// several rows: us a call in a graph, everything on, 8 x 48 rows of 151936 written with up to 1, 2, 4, 8 and 16 rows: 111, 90.2, 88.7, 87.7, 91.9;
+// ids only: 94.4, 77.3, 68.2, 67.4, 72.6.  Smaller calls have fewer by the rule; ids only, with LA_FILL 2048 (one row), 1024 (two), 512 (four) and
+// 256 (eight): 3 x up to 40 rows of 50257 12.4, 12.1, 14.8, 21.3; 64 rows of 128256 18.0, 16.2, 17.2, 20.1.  LA_QUADS 1 and 4: the first
+// call 92.2 and 92.6, the 3 x 40 rows 13.4 and 14.6.
 constexpr int LA_ROWS = 8;
 constexpr int64_t LA_FILL = 1024;
 typedef int32_t int4u __attribute__((ext_vector_type(4), aligned(4)));      // groups of four columns

@@ -16,7 +16,9 @@
 // Bound by the energy of its MFMAs and by issue slots: a stage of 64 tokens and 256 rows (D = 128) takes about 3390 cycles, 2056 of them the MFMAs',
 // at some 1.9 GHz.  1024 tokens of 40 heads behind 32768: 698 GFLOP, 621 us with the merge (1.12 PFLOP/s, where a library product of 8192^3 reaches 1.24);
 // a prompt of 4096 tokens, 32 heads: 141 us (0.98, half of the tiles' ends are masked).  D = 64 and caps have as many exponentials
-// for half the products, or two more instructions of that kind a score: 107 us for 84 GFLOP, 180 us for 134.
+// for half the products, or two more instructions of that kind a score: 107 us for 84 GFLOP, 180 us for 134.  Matrix cores and vector
+// instructions, which one wavefront a SIMD issues, hardly run beside each other: busy in 48 and 41 % of the cycles of the prompt of 4096, in 40
+// and 69 % with D = 64 (two wavefronts a SIMD), 36 and 57 % with a cap.
 #include "prompt_attn.h"
 
 namespace graft {
